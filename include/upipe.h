@@ -270,6 +270,52 @@ int upipe_rope(void* x, int64_t S, int H, int d, int64_t pos0, double base, int 
                hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * Rows of heads in a larger tensor, for the calls below: element (t, h, e) of
+ * [T, H, d] is the bf16 at p[t * row + h * head + e], strides in elements,
+ * multiples of 8, p 16-byte aligned.  Q, K and V may so be columns of one
+ * projection's output; a dense [T, H, d] has row = H d, head = d.  Rows that a call
+ * writes must not share elements with each other or with rows that it reads,
+ * other than as a call allows (UPIPE_ERR_INVALID_ARG).
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  void* p;
+  int64_t row, head;
+} upipe_heads;
+
+/* ------------------------------------------------------------------------
+ * RMS norm of every query and key head, and the rotary embedding at given
+ * positions behind it, in one pass (the attention of Qwen3-32B norms its heads
+ * so; packed sequences start their positions anew, which upipe_rope cannot).
+ *
+ *   q, k        bf16 [T, Hq, d], [T, Hkv, d]   projected rows
+ *   wq, wk      [d]    weights of the norms, bf16, or fp32 with w_fp32 = 1
+ *   positions   int64 [T]                      position of each row, dense
+ *   q_out, k_out                               out: the rows, normed and turned;
+ *                                              each may be q (k) itself
+ * Per row x:  y = R(position) (w x / sqrt(mean(x^2) + eps)), with the rotation R of
+ * upipe_rope, in fp32 with one rounding.  Positions of 0 .. 2^32 - 1 keep full accuracy;
+ * others are not looked for.  base must be finite and > 0, eps finite and > 0
+ * (UPIPE_ERR_INVALID_ARG), T < 2^31, Hq and Hkv 1 .. 64 (neither need divide the
+ * other), d = 128.  T = 0 is a no-op.  Needs no workspace.
+ * ---------------------------------------------------------------------- */
+int upipe_qk_norm_rope(upipe_heads q, upipe_heads k, const void* wq, const void* wk, int w_fp32,
+                       const int64_t* positions, upipe_heads q_out, upipe_heads k_out, int64_t T,
+                       int Hq, int Hkv, int d, double base, double eps, hipStream_t stream);
+
+/* Its gradients, from the same q, k, weights and positions:
+ *   dq_out, dk_out   upstream gradients of q_out, k_out
+ *   dq, dk           out: gradients of q, k; each may be dq_out (dk_out) or q (k)
+ *   dwq, dwk [d]     out, of the weights' type: summed over all rows, in an order
+ *                    that T, Hq and Hkv fix, and rounded once (T = 0: zeros)
+ * The workspace holds the partial sums of dwq and dwk. */
+size_t upipe_qk_norm_rope_bwd_workspace_size(int64_t T, int Hq, int Hkv, int d);
+int upipe_qk_norm_rope_bwd(upipe_heads q, upipe_heads k, const void* wq, const void* wk, int w_fp32,
+                           const int64_t* positions, upipe_heads dq_out, upipe_heads dk_out,
+                           upipe_heads dq, upipe_heads dk, void* dwq, void* dwk, int64_t T, int Hq,
+                           int Hkv, int d, double base, double eps, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * Attention block forward (Section 3.3, Appendix A "Untied Ulysses
  * (forward)"): QKV projection, attention written into `final_out`, output
  * projection y = final_out wo.  On one GPU all heads go through each step

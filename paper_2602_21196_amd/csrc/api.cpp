@@ -58,6 +58,7 @@ const char* const kFamilyNames[] = {
     "pack_rows",      "unpack_rows",   "rowdot_lse",     "attn_fwd",
     "attn_bwd_dkdv",  "attn_bwd_dq",   "gemm",           "gemm_wgrad",
     "reduce_splitk",  "lse_merge",     "rope",           "split_merge",
+    "norm_rope",      "norm_rope_bwd", "norm_dw_fold",
 };
 const int kNumFamilies = sizeof(kFamilyNames) / sizeof(kFamilyNames[0]);
 
@@ -98,6 +99,42 @@ bool group_split(int Hq, int Hkv, int U) {
   const int G = Hq / Hkv;
   for (int g = 0; g < Hkv; ++g)
     if ((g * G) / U != ((g + 1) * G - 1) / U) return true;
+  return false;
+}
+
+bool heads_ok(const upipe_heads& v, int64_t T, int H) {
+  const int64_t most = int64_t(1) << 60;
+  return aligned16(v.p) && v.row >= 0 && v.head >= 0 && v.row % 8 == 0 && v.head % 8 == 0 &&
+         v.row <= most / (T < 1 ? 1 : T) && v.head <= most / H;
+}
+
+static int64_t heads_span(const upipe_heads& v, int64_t T, int H) {   // elements
+  return (T - 1) * v.row + (H - 1) * v.head + HEAD_DIM;
+}
+
+bool heads_distinct(const upipe_heads& v, int64_t T, int H) {
+  if (T <= 1 && H <= 1) return true;
+  if (T <= 1) return v.head >= HEAD_DIM;
+  if (H <= 1) return v.row >= HEAD_DIM;
+  return (v.head >= HEAD_DIM && v.row >= (H - 1) * v.head + HEAD_DIM) ||
+         (v.row >= HEAD_DIM && v.head >= (T - 1) * v.row + HEAD_DIM);
+}
+
+bool heads_apart(const upipe_heads& a, int64_t Ta, int Ha, const upipe_heads& b, int64_t Tb,
+                 int Hb) {
+  if (Ta < 1 || Tb < 1) return true;
+  if (!overlap(a.p, 2 * heads_span(a, Ta, Ha), b.p, 2 * heads_span(b, Tb, Hb))) return true;
+  const int64_t d = ((int64_t)(uintptr_t)b.p - (int64_t)(uintptr_t)a.p) / 2;
+  if (a.row == b.row && a.row > 0) {
+    const int64_t sa = (Ha - 1) * a.head + HEAD_DIM, sb = (Hb - 1) * b.head + HEAD_DIM;
+    const int64_t at = ((d % a.row) + a.row) % a.row;
+    if (sa <= at && at + sb <= a.row) return true;
+  }
+  const int64_t h = a.head;
+  if (h == b.head && h >= 2 * HEAD_DIM && a.row % h == 0 && b.row % h == 0) {
+    const int64_t at = ((d % h) + h) % h;
+    if (at >= HEAD_DIM && at + HEAD_DIM <= h) return true;
+  }
   return false;
 }
 

@@ -4,6 +4,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/upipe.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -29,6 +30,9 @@ enum Family {
   kLseMerge,
   kRope,
   kSplitMerge,
+  kNormRope,
+  kNormRopeBwd,
+  kNormDwFold,
 };
 
 // Records HIP events around one launch when profiling is on.
@@ -68,6 +72,19 @@ constexpr int64_t kMaxRopePos = int64_t(1) << 32;
 int make_rope(double base, int64_t pos0, int64_t S, RopeArgs* out);
 int check_attn_shape(int64_t S, int Hq, int Hkv, int d, int U);
 bool group_split(int Hq, int Hkv, int U);
+
+// ---- rows that the caller places (upipe_heads) ------------------------------
+// Aligned, with strides of whole 16 bytes that reach no further than 2^60 elements.
+bool heads_ok(const upipe_heads& v, int64_t T, int H);
+// No two of the T x H rows share an element.
+bool heads_distinct(const upipe_heads& v, int64_t T, int H);
+// No row of a shares an element with one of b, as far as that shows: disjoint
+// ranges, columns of one row, or places of one head (K beside V in each).
+bool heads_apart(const upipe_heads& a, int64_t Ta, int Ha, const upipe_heads& b, int64_t Tb, int Hb);
+inline bool heads_same(const upipe_heads& a, const upipe_heads& b) {
+  return a.p == b.p && a.row == b.row && a.head == b.head;
+}
+inline HeadView view_of(const upipe_heads& v) { return HeadView{(bf16*)v.p, v.row, v.head, 0}; }
 
 // Bump allocator over the caller's workspace (256-byte aligned offsets).
 struct Carver {

@@ -136,4 +136,31 @@ int attn_bwd_dq_key_parts(int64_t S, int Hq, int causal);
 hipError_t launch_rope(bf16* x, int64_t S, int H, int64_t row, int64_t head,
                        RopeArgs rope, int inverse, hipStream_t st);
 
+// ---- norm of heads with rotation (norm_rope.hip) ---------------------------
+// Turns per position of the pairs e = 0 .. 63.
+struct NormFreq {
+  double turns[HEAD_DIM / 2];
+};
+struct NormRopeSide {      // q or k: rows x to y (backward: x and dy to y = dx)
+  HeadView x, dy, y;
+  const void* w;           // [128], bf16 or fp32
+  int H;
+};
+struct NormRopeArgs {
+  NormRopeSide q, k;
+  NormFreq freq;
+  const int64_t* positions;      // [T]
+  int64_t T;
+  float eps;
+  int w_fp32;
+  int blocks_q;      // set by the launcher
+};
+// y may be the rows of x (backward: of x or dy): a row is read before it is written.
+hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t st);
+// dx, and sums of dw to partial [norm_rope_bwd_partials][128] for launch_norm_dw_fold.
+int64_t norm_rope_bwd_partials(int64_t T, int Hq, int Hkv);
+hipError_t launch_norm_rope_bwd(NormRopeArgs a, float* partial, hipStream_t st);
+hipError_t launch_norm_dw_fold(const float* partial, int64_t T, int Hq, int Hkv, void* dwq,
+                               void* dwk, int w_fp32, hipStream_t st);
+
 }  // namespace upipe

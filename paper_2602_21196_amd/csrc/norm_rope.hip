@@ -1,0 +1,255 @@
+// RMS norm of every query and key head with the rotary embedding behind it, in
+// one pass, and its gradients.
+//
+// A row x of 128 elements (one head of one token) at position p, with weights w:
+//   r = (mean x^2 + eps)^(-1/2),   y = R(p) (r x w)
+// where R(p) turns the pairs (e, e + 64) as in upipe_rope.  Backward, from dy:
+//   g = R(p)^T dy,   a = g w,   dw += g n (over all rows),
+//   dx = r (a - n mean(a n)) with n = r x
+// r is formed again in the backward: it comes out of the row that is read anyway.
+//
+// HBM-bound: x is read and y written once (backward: x and dy read, dx written).
+// Eight lanes hold a row, lane j the elements 8j.. and 64 + 8j.., so a pair lies
+// in one lane and a wave reads whole 128-byte lines of 8 rows.  All rows (token,
+// head) of q, then those of k, are dealt out to workgroups, one tensor to each, so
+// a thread holds one tensor's 16 weights (and its 16 sums of dw).  The angles
+// are formed per row, in fp64 turns (positions to 2^32) with the frequencies from
+// the kernel's arguments: about a third of a row's instructions, under the time
+// that its bytes take.  The norm's sums, r, the rotation and the sums of dw are fp32; y, dx
+// and a bf16 dw are rounded once.
+#include "common.h"
+#include "kernels.h"
+
+namespace upipe {
+
+namespace {
+
+constexpr int kRowsPerBlock = 32;    // 256 threads, 8 lanes a row
+
+__device__ __forceinline__ float sum8(float v) {
+#pragma unroll
+  for (int off = 4; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+// A lane's 16 of a row's 128 elements.
+struct Row16 {
+  bf16x8 lo, hi;
+};
+__device__ __forceinline__ Row16 load_row(const bf16* p) {
+  return {*reinterpret_cast<const bf16x8*>(p), *reinterpret_cast<const bf16x8*>(p + 64)};
+}
+
+__device__ __forceinline__ void load_weights(const void* w, int w_fp32, int j, float (&out)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int at = 8 * j + (e & 7) + 64 * (e >> 3);
+    out[e] = w_fp32 ? static_cast<const float*>(w)[at]
+                    : (float)static_cast<const bf16*>(w)[at];
+  }
+}
+
+// The rows of one tensor that this lane group takes: r, r + step, ..., as (token,
+// head) without a division in the loop.
+struct RowWalk {
+  int64_t t, rows_left;
+  int h;
+  int64_t t_step;
+  int h_step, H;
+  __device__ __forceinline__ RowWalk(int64_t first, int64_t step, int64_t rows, int heads) {
+    H = heads;
+    t = first / heads;
+    h = (int)(first - t * heads);
+    t_step = step / heads;
+    h_step = (int)(step - t_step * heads);
+    rows_left = first < rows ? (rows - first + step - 1) / step : 0;
+  }
+  __device__ __forceinline__ void next() {
+    t += t_step;
+    h += h_step;
+    if (h >= H) {
+      h -= H;
+      ++t;
+    }
+    --rows_left;
+  }
+};
+
+__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
+  const bool is_q = (int)blockIdx.x < a.blocks_q;
+  const NormRopeSide& s = is_q ? a.q : a.k;
+  const int block = is_q ? blockIdx.x : blockIdx.x - a.blocks_q;
+  const int blocks = is_q ? a.blocks_q : gridDim.x - a.blocks_q;
+  const int j = threadIdx.x & 7;
+  RowWalk it((int64_t)block * kRowsPerBlock + (threadIdx.x >> 3), (int64_t)blocks * kRowsPerBlock,
+             a.T * s.H, s.H);
+  if (it.rows_left <= 0) return;
+  float w[16];
+  load_weights(s.w, a.w_fp32, j, w);
+  double f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = a.freq.turns[8 * j + e];
+  const bf16* x0 = s.x.p + 8 * j;
+  bf16* y0 = s.y.p + 8 * j;
+  for (; it.rows_left > 0; it.next()) {
+    const Row16 x = load_row(x0 + it.t * s.x.row + it.h * s.x.head);
+    const double pos = (double)a.positions[it.t];
+    float v[16], ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = (float)x.lo[e];
+      v[8 + e] = (float)x.hi[e];
+      ss = fmaf(v[e], v[e], ss);
+      ss = fmaf(v[8 + e], v[8 + e], ss);
+    }
+    const float r = __frsqrt_rn(fmaf(sum8(ss), 1.f / HEAD_DIM, a.eps));
+    Row16 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float c, sn;
+      const double turns = pos * f[e];
+      cos_sin_turns((float)(turns - rint(turns)), c, sn);
+      float p = v[e] * r * w[e], q = v[8 + e] * r * w[8 + e];
+      rope_pair(p, q, c, sn, false);
+      y.lo[e] = (bf16)p;
+      y.hi[e] = (bf16)q;
+    }
+    bf16* yp = y0 + it.t * s.y.row + it.h * s.y.head;
+    *reinterpret_cast<bf16x8*>(yp) = y.lo;
+    *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
+  }
+}
+
+// dx of every row, and each workgroup's sums of dw to partial[block][128].
+__global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeArgs a,
+                                                            float* __restrict__ partial) {
+  __shared__ float sums[4][HEAD_DIM];
+  const bool is_q = (int)blockIdx.x < a.blocks_q;
+  const NormRopeSide& s = is_q ? a.q : a.k;
+  const int block = is_q ? blockIdx.x : blockIdx.x - a.blocks_q;
+  const int blocks = is_q ? a.blocks_q : gridDim.x - a.blocks_q;
+  const int j = threadIdx.x & 7;
+  RowWalk it((int64_t)block * kRowsPerBlock + (threadIdx.x >> 3), (int64_t)blocks * kRowsPerBlock,
+             a.T * s.H, s.H);
+  float w[16], dw[16];
+  load_weights(s.w, a.w_fp32, j, w);
+  double f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = a.freq.turns[8 * j + e];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) dw[e] = 0.f;
+  const bf16* x0 = s.x.p + 8 * j;
+  const bf16* d0 = s.dy.p + 8 * j;
+  bf16* y0 = s.y.p + 8 * j;
+  for (; it.rows_left > 0; it.next()) {
+    const Row16 x = load_row(x0 + it.t * s.x.row + it.h * s.x.head);
+    const Row16 d = load_row(d0 + it.t * s.dy.row + it.h * s.dy.head);
+    const double pos = (double)a.positions[it.t];
+    float v[16], g[16], ss = 0.f, ax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e] = (float)x.lo[e];
+      v[8 + e] = (float)x.hi[e];
+      g[e] = (float)d.lo[e];
+      g[8 + e] = (float)d.hi[e];
+      float c, sn;
+      const double turns = pos * f[e];
+      cos_sin_turns((float)(turns - rint(turns)), c, sn);
+      rope_pair(g[e], g[8 + e], c, sn, true);
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      ss = fmaf(v[e], v[e], ss);
+      ax = fmaf(g[e] * w[e], v[e], ax);
+    }
+    const float r = __frsqrt_rn(fmaf(sum8(ss), 1.f / HEAD_DIM, a.eps));
+    const float m = sum8(ax) * r * (1.f / HEAD_DIM);      // mean(a r x)
+    Row16 y;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float n = v[e] * r;
+      dw[e] = fmaf(g[e], n, dw[e]);
+      const bf16 dx = (bf16)(r * fmaf(g[e], w[e], -n * m));
+      if (e < 8) y.lo[e] = dx;
+      else y.hi[e - 8] = dx;
+    }
+    bf16* yp = y0 + it.t * s.y.row + it.h * s.y.head;
+    *reinterpret_cast<bf16x8*>(yp) = y.lo;
+    *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
+  }
+  // The eight row groups of a wave, then the four waves, always in this order.
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+#pragma unroll
+    for (int off = 8; off <= 32; off <<= 1) dw[e] += __shfl_xor(dw[e], off);
+    if ((threadIdx.x & 56) == 0) sums[threadIdx.x >> 6][8 * j + (e & 7) + 64 * (e >> 3)] = dw[e];
+  }
+  __syncthreads();
+  const int e = threadIdx.x;
+  if (e < HEAD_DIM)
+    partial[(int64_t)blockIdx.x * HEAD_DIM + e] =
+        (sums[0][e] + sums[1][e]) + (sums[2][e] + sums[3][e]);
+}
+
+// dwq (blockIdx.y = 0) and dwk (1): the workgroups' sums added in fp64, in an order
+// that the sizes alone fix, and rounded once.  A workgroup takes 16 elements, 16
+// threads each.
+__global__ __launch_bounds__(256) void norm_dw_fold_kernel(const float* __restrict__ partial,
+                                                           int blocks_q, int blocks_k, void* dwq,
+                                                           void* dwk, int w_fp32) {
+  __shared__ double sums[16][17];
+  const int e = threadIdx.x & 15, p = threadIdx.x >> 4, at = blockIdx.x * 16 + e;
+  const bool is_q = blockIdx.y == 0;
+  const float* from = partial + (is_q ? 0 : (int64_t)blocks_q * HEAD_DIM) + at;
+  const int n = is_q ? blocks_q : blocks_k;
+  double sum = 0.0;
+  for (int b = p; b < n; b += 16) sum += (double)from[(int64_t)b * HEAD_DIM];
+  sums[p][e] = sum;
+  __syncthreads();
+  if (p > 0) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) sum += sums[i][e];
+  void* dw = is_q ? dwq : dwk;
+  if (w_fp32) static_cast<float*>(dw)[at] = (float)sum;
+  else static_cast<bf16*>(dw)[at] = (bf16)(float)sum;
+}
+
+}  // namespace
+
+// Workgroups of one tensor's rows: every row group has one row while that needs
+// no more than `most` workgroups.
+static int norm_blocks(int64_t rows, int most) {
+  const int64_t n = (rows + kRowsPerBlock - 1) / kRowsPerBlock;
+  return (int)(n < most ? n : most);
+}
+
+constexpr int kNormFwdBlocks = 4096, kNormBwdBlocks = 1024;
+
+hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t st) {
+  a.blocks_q = norm_blocks(a.T * a.q.H, kNormFwdBlocks);
+  const int blocks_k = norm_blocks(a.T * a.k.H, kNormFwdBlocks);
+  hipLaunchKernelGGL(norm_rope_kernel, dim3((unsigned)(a.blocks_q + blocks_k)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+int64_t norm_rope_bwd_partials(int64_t T, int Hq, int Hkv) {
+  return norm_blocks(T * Hq, kNormBwdBlocks) + norm_blocks(T * Hkv, kNormBwdBlocks);
+}
+
+hipError_t launch_norm_rope_bwd(NormRopeArgs a, float* partial, hipStream_t st) {
+  a.blocks_q = norm_blocks(a.T * a.q.H, kNormBwdBlocks);
+  const int blocks_k = norm_blocks(a.T * a.k.H, kNormBwdBlocks);
+  hipLaunchKernelGGL(norm_rope_bwd_kernel, dim3((unsigned)(a.blocks_q + blocks_k)), dim3(256), 0,
+                     st, a, partial);
+  return hipGetLastError();
+}
+
+hipError_t launch_norm_dw_fold(const float* partial, int64_t T, int Hq, int Hkv, void* dwq,
+                               void* dwk, int w_fp32, hipStream_t st) {
+  hipLaunchKernelGGL(norm_dw_fold_kernel, dim3(HEAD_DIM / 16, 2), dim3(256), 0, st, partial,
+                     norm_blocks(T * Hq, kNormBwdBlocks), norm_blocks(T * Hkv, kNormBwdBlocks), dwq,
+                     dwk, w_fp32);
+  return hipGetLastError();
+}
+
+}  // namespace upipe

@@ -27,6 +27,11 @@ _size = ctypes.c_size_t
 _fptr = ctypes.c_void_p
 _dbl = ctypes.c_double
 
+class upipe_heads(ctypes.Structure):
+    """Rows of heads in a larger tensor: pointer, row and head stride in elements."""
+    _fields_ = [("p", _c_void_p), ("row", _i64), ("head", _i64)]
+
+
 _SIGNATURES = {
     "upipe_status_string": (ctypes.c_char_p, [_int]),
     "upipe_version": (_int, []),
@@ -76,6 +81,14 @@ _SIGNATURES = {
                                   _c_void_p, _size, _c_void_p]),
     "upipe_gemm_bf16": (_int, [_c_void_p, _c_void_p, _c_void_p, _i64, _i64, _i64,
                                _c_void_p]),
+    "upipe_qk_norm_rope": (_int, [upipe_heads, upipe_heads, _c_void_p, _c_void_p, _int,
+                                  _c_void_p, upipe_heads, upipe_heads, _i64, _int, _int, _int,
+                                  _dbl, _dbl, _c_void_p]),
+    "upipe_qk_norm_rope_bwd_workspace_size": (_size, [_i64, _int, _int, _int]),
+    "upipe_qk_norm_rope_bwd": (_int, [upipe_heads, upipe_heads, _c_void_p, _c_void_p, _int,
+                                      _c_void_p] + [upipe_heads] * 4 +
+                               [_c_void_p, _c_void_p, _i64, _int, _int, _int, _dbl, _dbl,
+                                _c_void_p, _size, _c_void_p]),
     "upipe_profile_enable": (_int, [_int]),
     "upipe_profile_reset": (_int, []),
     "upipe_profile_query": (_int, [ctypes.c_char_p, ctypes.POINTER(_int),
@@ -228,6 +241,22 @@ def upipe_layer_bwd_ex(x, wqkv, wo, o_saved, lse_saved, dy, dx, dwqkv, dwo, B, S
 
 def upipe_gemm_bf16(a, b, c, M, N, K, stream):
     return lib().upipe_gemm_bf16(a, b, c, M, N, K, stream)
+
+
+def upipe_qk_norm_rope(q, k, wq, wk, w_fp32, positions, q_out, k_out, T, Hq, Hkv, d, base, eps,
+                       stream):
+    return lib().upipe_qk_norm_rope(q, k, wq, wk, w_fp32, positions, q_out, k_out, T, Hq, Hkv, d,
+                                    base, eps, stream)
+
+
+def upipe_qk_norm_rope_bwd_workspace_size(T, Hq, Hkv, d):
+    return lib().upipe_qk_norm_rope_bwd_workspace_size(T, Hq, Hkv, d)
+
+
+def upipe_qk_norm_rope_bwd(q, k, wq, wk, w_fp32, positions, dq_out, dk_out, dq, dk, dwq, dwk, T,
+                           Hq, Hkv, d, base, eps, ws, ws_bytes, stream):
+    return lib().upipe_qk_norm_rope_bwd(q, k, wq, wk, w_fp32, positions, dq_out, dk_out, dq, dk,
+                                        dwq, dwk, T, Hq, Hkv, d, base, eps, ws, ws_bytes, stream)
 
 
 def upipe_profile_enable(on):
@@ -535,3 +564,117 @@ def gemm(a, b):
                          _stream())
     _check("upipe_gemm_bf16", st)
     return c
+
+
+# ------------------------------------------- rows in place: strides, devices
+
+def _rows(t, name, shape=None):
+    """upipe_heads of a bf16 GPU tensor [T, H, 128] whose rows of 128 are dense: a
+    column block of a projection's output need not be copied."""
+    torch = _torch()
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [T,H,d], got {tuple(t.shape)}")
+    if shape is not None:
+        _shape(t, shape, name)
+    T, H, d = t.shape
+    if d > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name} must have dense rows, got strides {t.stride()}")
+    head = t.stride(1) if H > 1 else d
+    row = t.stride(0) if T > 1 else H * head
+    return upipe_heads(t.data_ptr(), row, head)
+
+
+class _Call:
+    """The device of a call's tensors, made the current one around it, and its
+    current stream; every tensor of the call has to be on it."""
+
+    def __init__(self, **tensors):
+        devices = {t.device for t in tensors.values() if t is not None}
+        if len(devices) != 1:
+            raise ValueError("tensors on different devices: " + ", ".join(
+                f"{n} on {t.device}" for n, t in tensors.items() if t is not None))
+        self.device = devices.pop()
+        self._at = _torch().cuda.device(self.device)
+
+    def __enter__(self):
+        self._at.__enter__()
+        return _stream()
+
+    def __exit__(self, *exc):
+        return self._at.__exit__(*exc)
+
+
+def _workspace(ws, need, device, fn):
+    """ws checked, or a new one of `need` bytes."""
+    if need == 0:
+        raise UpipeError(fn, -1)
+    if ws is None:
+        return workspace(need, device)
+    _ptr(ws, _torch().uint8, "ws")
+    return ws
+
+
+# ----------------------------------------------- norm of heads with rotation
+
+def _norm_inputs(q, k, wq, wk, positions):
+    """(T, Hq, Hkv, views of q and k, pointers of weights and positions, fp32?)"""
+    torch = _torch()
+    vq = _rows(q, "q")
+    T, Hq, d = q.shape
+    vk = _rows(k, "k", (T, k.shape[1] if k.dim() == 3 else 1, d))
+    if wq.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"wq must be bfloat16 or float32, got {wq.dtype}")
+    _shape(wq, (d,), "wq")
+    _shape(wk, (d,), "wk")
+    _shape(positions, (T,), "positions")
+    return (T, Hq, k.shape[1], vq, vk,
+            (_ptr(wq, wq.dtype, "wq"), _ptr(wk, wq.dtype, "wk"),
+             int(wq.dtype == torch.float32), _ptr(positions, torch.int64, "positions")))
+
+
+def _pair_out(out, shapes, device, names):
+    """The caller's two output tensors, or two new dense ones."""
+    if out is None:
+        torch = _torch()
+        return tuple(torch.empty(s, dtype=torch.bfloat16, device=device) for s in shapes)
+    for t, s, n in zip(out, shapes, names):
+        _rows(t, n, s)
+    return tuple(out)
+
+
+def qk_norm_rope(q, k, wq, wk, positions, base, eps=1e-6, out=None):
+    """(q', k'): every head of q [T,Hq,d] and k [T,Hkv,d] normed over its d
+    elements, times wq / wk [d] (bf16 or fp32), rotated at positions [T] (int64).
+    q, k and out = (q', k') may be strided views with dense rows; out may be (q, k)."""
+    T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
+    yq, yk = _pair_out(out, (tuple(q.shape), tuple(k.shape)), q.device, ("q_out", "k_out"))
+    with _Call(q=q, k=k, wq=wq, wk=wk, positions=positions, q_out=yq, k_out=yk) as stream:
+        st = upipe_qk_norm_rope(vq, vk, *rest, _rows(yq, "q_out"), _rows(yk, "k_out"), T, Hq, Hkv,
+                                q.shape[2], float(base), float(eps), stream)
+    _check("upipe_qk_norm_rope", st)
+    return yq, yk
+
+
+def qk_norm_rope_bwd(q, k, wq, wk, positions, base, dq_out, dk_out, eps=1e-6, out=None, ws=None):
+    """(dq, dk, dwq, dwk) from the inputs of qk_norm_rope and the gradients of its
+    outputs.  out = (dq, dk) may be (dq_out, dk_out) or (q, k)."""
+    torch = _torch()
+    T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
+    vdq, vdk = _rows(dq_out, "dq_out", q.shape), _rows(dk_out, "dk_out", k.shape)
+    dq, dk = _pair_out(out, (tuple(q.shape), tuple(k.shape)), q.device, ("dq", "dk"))
+    dwq, dwk = torch.empty_like(wq), torch.empty_like(wk)
+    ws = _workspace(ws, upipe_qk_norm_rope_bwd_workspace_size(T, Hq, Hkv, q.shape[2]), q.device,
+                    "upipe_qk_norm_rope_bwd_workspace_size")
+    with _Call(q=q, k=k, wq=wq, wk=wk, positions=positions, dq_out=dq_out, dk_out=dk_out, dq=dq,
+               dk=dk, ws=ws) as stream:
+        st = upipe_qk_norm_rope_bwd(vq, vk, *rest, vdq, vdk, _rows(dq, "dq"), _rows(dk, "dk"),
+                                    dwq.data_ptr(), dwk.data_ptr(), T, Hq, Hkv, q.shape[2],
+                                    float(base), float(eps), ws.data_ptr(), ws.numel(), stream)
+    _check("upipe_qk_norm_rope_bwd", st)
+    return dq, dk, dwq, dwk
