@@ -283,6 +283,71 @@ typedef struct {
 } upipe_heads;
 
 /* ------------------------------------------------------------------------
+ * Attention over packed sequences of different lengths.
+ *
+ * n_seq sequences lie one behind the other: sequence s has the query rows
+ * [cu_q[s], cu_q[s+1]) and the key/value rows [cu_k[s], cu_k[s+1]), either of which
+ * may be none.  Its queries are the last ones of its keys: with causal = 1 query i
+ * sees key j iff j <= i + Lk - Lq (Lq, Lk its lengths), with causal = 0 every key
+ * of the sequence.  A query that sees no key gets o = 0, lse = -inf and
+ * gradients of 0; a key that no query sees gets gradients of 0.
+ *
+ * The plan: cu_q and cu_k are HOST arrays of n_seq + 1 offsets, 0 first, none less
+ * than the one before.  upipe_varlen_plan writes the plan of these lengths and head
+ * counts to host memory (8-byte aligned, of upipe_varlen_plan_size bytes; 0: invalid
+ * or unsupported lengths); the caller copies the bytes to the device (16-byte
+ * aligned).  The calls below take both: `plan` is read on the host, during the
+ * call only, `plan_dev` by the kernels.  A plan serves any number of calls, on any
+ * stream, also at once; a captured call keeps the list of work that it was captured
+ * with.  Hkv | Hq <= 64, d = 128, up to 2^20 sequences of lengths up to 2^24 - 128.
+ *
+ *   q, o   rows [.., Hq, d], k, v rows [.., Hkv, d], up to the last offset at least;
+ *          rows behind it are neither read nor written.  Rows of k and v are at
+ *          most 2^22 elements apart (UPIPE_ERR_UNSUPPORTED).  o may be q itself.
+ *   lse    fp32, head h of query row t at lse[h * lse_head + t]
+ * Scores, softmax and sums are fp32; the weights are rounded to bf16 for their product
+ * with v.  lse carries no rounding to bf16.  A masked value that is infinite or
+ * not a number does not reach a row; a visible one does.  The results depend on the lengths
+ * and head counts of the whole plan in their last bits.
+ * ---------------------------------------------------------------------- */
+size_t upipe_varlen_plan_size(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int Hq, int Hkv,
+                              int d, int causal);
+int upipe_varlen_plan(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int Hq, int Hkv, int d,
+                      int causal, void* plan, size_t plan_bytes);
+size_t upipe_attn_fwd_varlen_workspace_size(const void* plan);
+int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_heads o, float* lse,
+                          int64_t lse_head, const void* plan, const void* plan_dev, void* ws,
+                          size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Attention of a few new tokens of every sequence against its cache, and against
+ * a prefix that all sequences share.
+ *
+ *   q, o   rows [B nq, Hq, d]: token t of sequence b is row b nq + t; o may be q
+ *   k, v   rows [cap, Hkv, d] of cache 0; cache b lies b * k_cache (v_cache)
+ *          elements on
+ *   lens   int32 [B] on the DEVICE: valid rows of each cache, the nq new ones
+ *          among them; values outside 0 .. cap are taken as the nearer of these.
+ *          Rows from lens[b] on are not read.
+ *   k_prefix, v_prefix  rows [P, Hkv, d] that stand before the rows of every cache;
+ *          not looked at with P = 0
+ *   lse    fp32 [B, Hq, nq]
+ * Token t of b sees the whole prefix and the rows j <= t + lens[b] - nq of its cache (none of
+ * them if lens[b] + t < nq; with no key at all o = 0, lse = -inf).  The prefix is
+ * read for all sequences together, and its weights join the cache's by
+ * log-sum-exps in fp32.  How rows are split follows from B, nq, cap, P and the head counts,
+ * never from lens, so a captured call may be replayed as the caches grow.  nq <= 128,
+ * B <= 65536, cap and P up to 2^24 - 128, rows of k, v and the prefix at most 2^22
+ * elements apart.  Numerics as above.
+ * ---------------------------------------------------------------------- */
+size_t upipe_attn_decode_workspace_size(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv,
+                                        int d);
+int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads v, int64_t v_cache,
+                      const int32_t* lens, upipe_heads k_prefix, upipe_heads v_prefix,
+                      upipe_heads o, float* lse, int64_t B, int nq, int64_t cap, int64_t P, int Hq,
+                      int Hkv, int d, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * RMS norm of every query and key head, and the rotary embedding at given
  * positions behind it, in one pass (the attention of Qwen3-32B norms its heads
  * so; packed sequences start their positions anew, which upipe_rope cannot).

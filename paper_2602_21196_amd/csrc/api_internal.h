@@ -33,6 +33,12 @@ enum Family {
   kNormRope,
   kNormRopeBwd,
   kNormDwFold,
+  kRowsFwd,
+  kRowsMerge,
+  kRowsTerms,
+  kRowsDkdv,
+  kRowsDkdvFold,
+  kRowsDq,
 };
 
 // Records HIP events around one launch when profiling is on.

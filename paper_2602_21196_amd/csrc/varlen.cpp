@@ -1,0 +1,483 @@
+// Entry points of attention over packed sequences and caches (declared in
+// include/upipe.h), and the host's plan of their work.
+//
+// A plan lists every workgroup's work for one batch of lengths, longest first: the
+// sequences differ in length, so a grid over the longest one would mostly be empty,
+// and which tiles are long is not where the device can sort them for free.  A
+// training step's layers, forward and backward, share one plan.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <functional>
+#include <queue>
+#include <vector>
+
+#include "../../include/upipe.h"
+#include "api_internal.h"
+#include "kernels.h"
+#include "varlen.h"
+
+namespace upipe {
+
+namespace {
+
+constexpr uint64_t kPlanMagic = 0x31306e6c70727670ull;
+constexpr int kMaxSequences = 1 << 20;
+constexpr int64_t kMaxTokens = int64_t(1) << 40;
+// Elements from one token's row to the next: a stage of 128 rows is addressed with
+// 32-bit byte offsets.
+constexpr int64_t kMaxRowStride = int64_t(1) << 22;
+constexpr int64_t kMaxGrid = int64_t(1) << 30;
+constexpr int kCUs = 256;
+
+// Time at which the last of these workgroups ends: each goes to the first of the CUs
+// that is free, in order, one to a CU.
+double makespan(const std::vector<float>& cost, int copies) {
+  std::priority_queue<double, std::vector<double>, std::greater<double>> free;
+  for (int i = 0; i < kCUs; ++i) free.push(0.0);
+  double end = 0.0;
+  for (float c : cost)
+    for (int i = 0; i < copies; ++i) {
+      const double t = free.top() + c;
+      free.pop();
+      free.push(t);
+      end = std::max(end, t);
+    }
+  return end;
+}
+
+struct Lengths {
+  int64_t q0, k0;
+  int32_t Lq, Lk;
+};
+
+// us of one 128-key stage of a forward workgroup with 1, 2, 4 key parts on a full
+// chip, and of a workgroup besides its stages.
+constexpr double kFwdStage[3] = {3.5, 2.0, 1.2}, kFwdFixed = 3.0;
+constexpr int kFwdParts[3] = {1, 2, 4};
+// us that a merge launch takes, and that it takes for one part of 64 rows.
+constexpr double kMergeFixed = 4.0, kMergePart = 0.01;
+
+struct FwdChoice {
+  int ks = 1;
+  int most = 1 << 30;      // stages of a part
+  double est = 0.0;
+};
+
+int row_tiles(int32_t Lq, int G, int rows) { return (int)(((int64_t)Lq * G + rows - 1) / rows); }
+
+// Stages of tile `tile` of `rows` packed rows.
+int tile_stages(const Lengths& s, int G, int rows, int tile, int causal) {
+  const int64_t last = (std::min<int64_t>((int64_t)(tile + 1) * rows, (int64_t)s.Lq * G) - 1) / G;
+  const int64_t seen = causal ? std::min<int64_t>(s.Lk, last + 1 + s.Lk - s.Lq) : s.Lk;
+  return seen <= 0 ? 0 : (int)((seen + 127) / 128);
+}
+
+// Parts into which the keys of a sequence's tiles are cut so that none has more
+// than `most` stages.
+int seq_parts(const Lengths& s, int most) { return s.Lk <= 0 ? 1 : ((s.Lk + 127) / 128 + most - 1) / most; }
+
+struct FwdWork {
+  RowItem item;
+  int stages, seq;
+};
+
+void fwd_work(const std::vector<Lengths>& seqs, int G, int causal, const FwdChoice& c,
+              std::vector<FwdWork>* out) {
+  const int rows = 256 / c.ks;
+  out->clear();
+  for (size_t i = 0; i < seqs.size(); ++i) {
+    const Lengths& s = seqs[i];
+    const int np = seq_parts(s, c.most), n = row_tiles(s.Lq, G, rows);
+    for (int t = n - 1; t >= 0; --t) {
+      const int st = tile_stages(s, G, rows, t, causal), per = (st + np - 1) / np;
+      for (int p = 0; p < np; ++p) {
+        RowItem it{};
+        it.q0 = s.q0;
+        it.k0 = s.k0;
+        it.Lq = s.Lq;
+        it.Lk = s.Lk;
+        it.tile = t;
+        it.part = p;
+        it.parts = np;
+        out->push_back({it, std::max(0, std::min(st, per * (p + 1)) - per * p), (int)i});
+      }
+    }
+  }
+  std::stable_sort(out->begin(), out->end(),
+                   [](const FwdWork& a, const FwdWork& b) { return a.stages > b.stages; });
+}
+
+// The split of waves (1, 2 or 4 parts of a stage's keys) and of keys over
+// workgroups whose list is expected to end first.  Long lists need no look: from 16
+// workgroups a CU on the largest tiles are the fastest.
+FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
+  FwdChoice best;
+  int64_t tiles = 0;
+  for (const Lengths& s : seqs) tiles += row_tiles(s.Lq, G, 256);
+  if (tiles * Hkv >= 16 * kCUs) return best;
+  std::vector<FwdWork> work;
+  std::vector<float> cost;
+  bool first = true;
+  auto look = [&](FwdChoice c, int i) {
+    fwd_work(seqs, G, causal, c, &work);
+    cost.clear();
+    int64_t parts = 0, stages = 0;
+    for (const FwdWork& w : work) {
+      cost.push_back((float)(kFwdFixed + w.stages * kFwdStage[i]));
+      parts += w.item.parts > 1;
+      stages += w.stages;
+    }
+    c.est = makespan(cost, Hkv);
+    if (parts > 0) c.est += kMergeFixed + kMergePart * parts * Hkv * (4.0 / c.ks);
+    // parts take workspace: only for a gain
+    if (first || c.est < (parts > 0 ? 0.95 : 1.0) * best.est) best = c;
+    first = false;
+    return stages * Hkv;
+  };
+  for (int i = 0; i < 3; ++i) {
+    FwdChoice c;
+    c.ks = kFwdParts[i];
+    const int64_t mean = (look(c, i) + kCUs - 1) / kCUs;      // stages of a CU
+    for (int64_t m : {mean, 2 * mean}) {
+      c.most = (int)std::max<int64_t>(4, m);
+      look(c, i);
+    }
+  }
+  return best;
+}
+
+int check_lengths(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, int d, int causal,
+                  std::vector<Lengths>* seqs) {
+  if (n < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || !cu_q || !cu_k || (causal != 0 && causal != 1))
+    return UPIPE_ERR_INVALID_ARG;
+  if (d != HEAD_DIM || Hq > kMaxHeads || n > kMaxSequences) return UPIPE_ERR_UNSUPPORTED;
+  if (cu_q[0] != 0 || cu_k[0] != 0) return UPIPE_ERR_INVALID_ARG;
+  seqs->resize(n);
+  for (int i = 0; i < n; ++i) {
+    if (cu_q[i + 1] < cu_q[i] || cu_k[i + 1] < cu_k[i]) return UPIPE_ERR_INVALID_ARG;
+    const int64_t Lq = cu_q[i + 1] - cu_q[i], Lk = cu_k[i + 1] - cu_k[i];
+    if (Lq > kMaxSeq || Lk > kMaxSeq || cu_q[i + 1] >= kMaxTokens || cu_k[i + 1] >= kMaxTokens)
+      return UPIPE_ERR_UNSUPPORTED;
+    (*seqs)[i] = {cu_q[i], cu_k[i], (int32_t)Lq, (int32_t)Lk};
+  }
+  return UPIPE_OK;
+}
+
+struct Plan {
+  PlanHeader h{};
+  std::vector<RowItem> fwd;
+  std::vector<MergeItem> merge;
+};
+
+template <class T>
+int64_t place(int64_t* end, const std::vector<T>& v) {
+  const int64_t at = *end;
+  *end = round_up(at + (int64_t)(v.size() * sizeof(T)), 64);
+  return at;
+}
+
+int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, int d, int causal,
+              Plan* p) {
+  std::vector<Lengths> seqs;
+  const int rc = check_lengths(cu_q, cu_k, n, Hq, Hkv, d, causal, &seqs);
+  if (rc != UPIPE_OK) return rc;
+  const int G = Hq / Hkv;
+  PlanHeader& h = p->h;
+  h.magic = kPlanMagic;
+  h.n_seq = n;
+  h.Hq = Hq;
+  h.Hkv = Hkv;
+  h.causal = causal;
+  h.total_q = cu_q[n];
+  h.total_k = cu_k[n];
+  for (const Lengths& s : seqs) {
+    h.longest_q = std::max<int64_t>(h.longest_q, s.Lq);
+    h.longest_k = std::max<int64_t>(h.longest_k, s.Lk);
+  }
+
+  const FwdChoice c = choose_fwd(seqs, G, Hkv, causal);
+  std::vector<FwdWork> work;
+  fwd_work(seqs, G, causal, c, &work);
+  h.fwd_ks = c.ks;
+  // Partial rows: [parts][Lq][Hq] of every sequence that is cut.
+  std::vector<int64_t> p0;
+  for (const Lengths& s : seqs) {
+    const int np = seq_parts(s, c.most);
+    p0.push_back(h.part_rows);
+    if (np < 2 || s.Lq < 1) continue;
+    const int64_t rows = (int64_t)s.Lq * Hq;
+    for (int64_t b = 0; b < (rows + 15) / 16; ++b)
+      p->merge.push_back({s.q0, h.part_rows, s.Lq, np, (int32_t)b, 0});
+    h.part_rows += np * rows;
+  }
+  for (FwdWork& w : work) {
+    w.item.p0 = p0[w.seq];
+    p->fwd.push_back(w.item);
+  }
+
+  if ((int64_t)p->fwd.size() * Hkv > kMaxGrid || (int64_t)p->merge.size() > kMaxGrid)
+    return UPIPE_ERR_UNSUPPORTED;
+  h.n_fwd = (int32_t)p->fwd.size();
+  h.n_merge = (int32_t)p->merge.size();
+  int64_t end = round_up(sizeof(PlanHeader), 64);
+  h.at_fwd = place(&end, p->fwd);
+  h.at_merge = place(&end, p->merge);
+  h.bytes = end;
+  return UPIPE_OK;
+}
+
+template <class T>
+void put(char* to, int64_t at, const std::vector<T>& v) {
+  if (!v.empty()) memcpy(to + at, v.data(), v.size() * sizeof(T));
+}
+
+const PlanHeader* header_of(const void* plan) {
+  const PlanHeader* h = (const PlanHeader*)plan;
+  return plan && ((uintptr_t)plan & 7) == 0 && h->magic == kPlanMagic ? h : nullptr;
+}
+
+size_t parts_bytes(int64_t rows) { return (size_t)rows * (HEAD_DIM + 1) * 4; }
+
+size_t fwd_ws(const PlanHeader& h) { return parts_bytes(h.part_rows) + 16; }
+
+bool stage_rows(const upipe_heads& v) { return v.row <= kMaxRowStride; }
+
+// Rows that a call writes, apart from those that it reads (T rows each).
+bool apart(const upipe_heads& out, int64_t To, int Ho, const upipe_heads& in, int64_t Ti, int Hi) {
+  return heads_apart(out, To, Ho, in, Ti, Hi);
+}
+
+}  // namespace
+
+}  // namespace upipe
+
+using namespace upipe;
+
+extern "C" {
+
+size_t upipe_varlen_plan_size(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int Hq, int Hkv,
+                              int d, int causal) {
+  try {
+    Plan p;
+    return make_plan(cu_q, cu_k, n_seq, Hq, Hkv, d, causal, &p) == UPIPE_OK ? (size_t)p.h.bytes : 0;
+  } catch (...) {
+    return 0;
+  }
+}
+
+int upipe_varlen_plan(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int Hq, int Hkv, int d,
+                      int causal, void* plan, size_t plan_bytes) {
+  try {
+    if (!plan || ((uintptr_t)plan & 7) != 0) return UPIPE_ERR_INVALID_ARG;
+    Plan p;
+    const int rc = make_plan(cu_q, cu_k, n_seq, Hq, Hkv, d, causal, &p);
+    if (rc != UPIPE_OK) return rc;
+    if (plan_bytes < (size_t)p.h.bytes) return UPIPE_ERR_WORKSPACE;
+    char* to = (char*)plan;
+    memset(to, 0, p.h.bytes);
+    memcpy(to, &p.h, sizeof(p.h));
+    put(to, p.h.at_fwd, p.fwd);
+    put(to, p.h.at_merge, p.merge);
+    return UPIPE_OK;
+  } catch (...) {
+    return UPIPE_ERR_HIP;
+  }
+}
+
+size_t upipe_attn_fwd_varlen_workspace_size(const void* plan) {
+  const PlanHeader* h = header_of(plan);
+  return h ? fwd_ws(*h) : 0;
+}
+
+int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_heads o, float* lse,
+                          int64_t lse_head, const void* plan, const void* plan_dev, void* ws,
+                          size_t ws_bytes, hipStream_t stream) {
+  try {
+    const PlanHeader* h = header_of(plan);
+    if (!h || !aligned16(plan_dev)) return UPIPE_ERR_INVALID_ARG;
+    const int64_t Tq = h->total_q, Tk = h->total_k;
+    const int Hq = h->Hq, Hkv = h->Hkv;
+    if (Tq == 0) return UPIPE_OK;
+    if (!aligned16(lse) || !aligned16(ws)) return UPIPE_ERR_INVALID_ARG;
+    if (lse_head < Tq || lse_head > kMaxTokens) return UPIPE_ERR_INVALID_ARG;
+    if (!heads_ok(q, Tq, Hq) || !heads_ok(o, Tq, Hq) || !heads_distinct(o, Tq, Hq) ||
+        (Tk > 0 && (!heads_ok(k, Tk, Hkv) || !heads_ok(v, Tk, Hkv))))
+      return UPIPE_ERR_INVALID_ARG;
+    // o may be q: a workgroup reads its rows before it writes them.
+    if ((!heads_same(o, q) && !apart(o, Tq, Hq, q, Tq, Hq)) || !apart(o, Tq, Hq, k, Tk, Hkv) ||
+        !apart(o, Tq, Hq, v, Tk, Hkv))
+      return UPIPE_ERR_INVALID_ARG;
+    if (!stage_rows(k) || !stage_rows(v)) return UPIPE_ERR_UNSUPPORTED;
+    if (ws_bytes < fwd_ws(*h)) return UPIPE_ERR_WORKSPACE;
+    RowFwdArgs a{};
+    a.q = view_of(q);
+    a.k = view_of(k);
+    a.v = view_of(v);
+    a.o = view_of(o);
+    a.lse = lse;
+    a.lse_head = lse_head;
+    a.part_o = (float*)ws;
+    a.part_lse = a.part_o + h->part_rows * HEAD_DIM;
+    a.items = (const RowItem*)((const char*)plan_dev + h->at_fwd);
+    a.Hkv = Hkv;
+    a.G = Hq / Hkv;
+    a.causal = h->causal;
+    UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsPlanned, h->fwd_ks, a, h->n_fwd, stream));
+    if (h->n_merge > 0) {
+      RowMergeArgs m{};
+      m.part_o = a.part_o;
+      m.part_lse = a.part_lse;
+      m.o = a.o;
+      m.lse = lse;
+      m.lse_head = lse_head;
+      m.items = (const MergeItem*)((const char*)plan_dev + h->at_merge);
+      m.Hq = Hq;
+      UPIPE_LAUNCH(kRowsMerge, stream, launch_rows_merge(m, h->n_merge, stream));
+    }
+    return UPIPE_OK;
+  } catch (...) {
+    return UPIPE_ERR_HIP;
+  }
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- caches
+namespace upipe {
+
+namespace {
+
+// How a call over caches is cut: key parts of every row, and of the prefix.
+struct CachePlan {
+  int splits = 1;
+  int prefix_ks = 1, prefix_parts = 0;
+  int64_t rows = 0;        // B * nq * Hq
+};
+
+int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int d) {
+  if (B < 1 || nq < 1 || cap < 1 || P < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0)
+    return UPIPE_ERR_INVALID_ARG;
+  if (d != HEAD_DIM || Hq > kMaxHeads || cap > kMaxSeq || P > kMaxSeq || nq > 128 || B > 65536)
+    return UPIPE_ERR_UNSUPPORTED;
+  return UPIPE_OK;
+}
+
+// The lengths are on the device: the cut goes by the capacity, and a part is the
+// same share of whatever a cache holds.  About four workgroups a CU even out caches of
+// different lengths; a part has four stages of 128 rows at least, as long as the
+// cache is full.
+CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv) {
+  CachePlan p;
+  p.rows = B * nq * Hq;
+  const int64_t G = Hq / Hkv, tiles = (nq * G + 63) / 64, groups = B * Hkv * tiles;
+  const int64_t stages = (cap + 127) / 128;
+  p.splits = (int)std::max<int64_t>(1, std::min((4 * kCUs + groups - 1) / groups, (stages + 3) / 4));
+  if (P > 0) {
+    const int64_t rows = B * nq * G, ps = (P + 127) / 128;
+    p.prefix_ks = rows > 128 ? 1 : rows > 64 ? 2 : 4;
+    const int64_t n = (rows * p.prefix_ks + 255) / 256 * Hkv;
+    p.prefix_parts = (int)std::max<int64_t>(1, std::min((kCUs + n - 1) / n, (ps + 1) / 2));
+  }
+  return p;
+}
+
+// The rows of o outside the range of all caches.
+bool apart_cache(const upipe_heads& o, int64_t T, int Hq, const upipe_heads& k, int64_t batch, int64_t B,
+                 int64_t cap, int Hkv) {
+  const int64_t so = (T - 1) * o.row + (Hq - 1) * o.head + HEAD_DIM;
+  const int64_t sk = (B - 1) * batch + (cap - 1) * k.row + (Hkv - 1) * k.head + HEAD_DIM;
+  return !overlap(o.p, 2 * so, k.p, 2 * sk);
+}
+
+int64_t cache_parts(const CachePlan& p) { return p.splits + p.prefix_parts; }
+
+}  // namespace
+
+}  // namespace upipe
+
+extern "C" {
+
+size_t upipe_attn_decode_workspace_size(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv,
+                                        int d) {
+  if (check_cache(B, nq, cap, P, Hq, Hkv, d) != UPIPE_OK) return 0;
+  const CachePlan p = plan_cache(B, nq, cap, P, Hq, Hkv);
+  return parts_bytes(cache_parts(p) * p.rows) + 16;
+}
+
+int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads v, int64_t v_cache,
+                      const int32_t* lens, upipe_heads k_prefix, upipe_heads v_prefix, upipe_heads o,
+                      float* lse, int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int d,
+                      void* ws, size_t ws_bytes, hipStream_t stream) {
+  try {
+    const int rc = check_cache(B, nq, cap, P, Hq, Hkv, d);
+    if (rc != UPIPE_OK) return rc;
+    const int64_t T = B * nq, most = int64_t(1) << 60;
+    if (!heads_ok(q, T, Hq) || !heads_ok(o, T, Hq) || !heads_distinct(o, T, Hq) ||
+        !heads_ok(k, cap, Hkv) || !heads_ok(v, cap, Hkv) || !lens || ((uintptr_t)lens & 3) != 0 || !aligned16(lse) ||
+        !aligned16(ws) || k_cache < 0 || v_cache < 0 || k_cache % 8 != 0 || v_cache % 8 != 0 ||
+        k_cache > most / B || v_cache > most / B)
+      return UPIPE_ERR_INVALID_ARG;
+    if (P > 0 && (!heads_ok(k_prefix, P, Hkv) || !heads_ok(v_prefix, P, Hkv)))
+      return UPIPE_ERR_INVALID_ARG;
+    if ((!heads_same(o, q) && !apart(o, T, Hq, q, T, Hq)) || !apart_cache(o, T, Hq, k, k_cache, B, cap, Hkv) ||
+        !apart_cache(o, T, Hq, v, v_cache, B, cap, Hkv) ||
+        (P > 0 && (!apart(o, T, Hq, k_prefix, P, Hkv) || !apart(o, T, Hq, v_prefix, P, Hkv))))
+      return UPIPE_ERR_INVALID_ARG;
+    if (!stage_rows(k) || !stage_rows(v) || (P > 0 && (!stage_rows(k_prefix) || !stage_rows(v_prefix))))
+      return UPIPE_ERR_UNSUPPORTED;
+    if (ws_bytes < upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d))
+      return UPIPE_ERR_WORKSPACE;
+    const CachePlan p = plan_cache(B, nq, cap, P, Hq, Hkv);
+    const int G = Hq / Hkv;
+    RowFwdArgs a{};
+    a.q = view_of(q);
+    a.o = view_of(o);
+    a.lse = lse;
+    a.part_o = (float*)ws;
+    a.part_lse = a.part_o + cache_parts(p) * p.rows * HEAD_DIM;
+    a.Hkv = Hkv;
+    a.G = G;
+    if (P > 0) {
+      a.k = view_of(k_prefix);
+      a.v = view_of(v_prefix);
+      a.one.Lq = (int32_t)T;
+      a.one.Lk = (int32_t)P;
+      a.one.parts = p.prefix_parts;
+      a.causal = 0;
+      const int64_t tiles = (T * G * p.prefix_ks + 255) / 256;
+      UPIPE_LAUNCH(kRowsFwd, stream,
+                   launch_rows_fwd(kRowsOne, p.prefix_ks, a, tiles * p.prefix_parts, stream));
+    }
+    a.k = view_of(k);
+    a.v = view_of(v);
+    a.k.batch = k_cache;
+    a.v.batch = v_cache;
+    a.lens = lens;
+    a.cap = cap;
+    a.causal = 1;
+    a.B = (int)B;
+    a.nq = nq;
+    a.splits = p.splits;
+    a.part0 = p.prefix_parts;
+    const int64_t tiles = ((int64_t)nq * G + 63) / 64;
+    UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, a, tiles * B * p.splits, stream));
+    RowMergeArgs m{};
+    m.part_o = a.part_o;
+    m.part_lse = a.part_lse;
+    m.o = a.o;
+    m.lse = lse;
+    m.rows = p.rows;
+    m.Hq = Hq;
+    m.parts = (int)cache_parts(p);
+    m.nq = nq;
+    UPIPE_LAUNCH(kRowsMerge, stream, launch_rows_merge(m, 0, stream));
+    return UPIPE_OK;
+  } catch (...) {
+    return UPIPE_ERR_HIP;
+  }
+}
+
+}  // extern "C"

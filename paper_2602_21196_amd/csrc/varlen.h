@@ -1,0 +1,96 @@
+// Attention over packed sequences and over caches: what the host plans and the
+// kernels read (varlen.cpp, varlen_fwd.hip, varlen_bwd.hip).
+//
+// Rows are packed by key/value group: row r of a sequence and a key/value head is
+// query token r / G under the group's head r % G (G = Hq / Hkv).  The rows of a
+// group share their keys, so a workgroup's tile of rows covers few tokens: a
+// single token fills G rows, a short sequence wastes less of a tile, and the
+// diagonal is cut finer.
+#pragma once
+#include <stdint.h>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace upipe {
+
+// One workgroup's rows of the forward (or of dQ): tile `tile` of a sequence, part
+// `part` of its keys.  Parts leave fp32 results at rows p0 + part * Lq * Hq + ...
+struct RowItem {
+  int64_t q0, k0, p0;      // first query row, key row, partial row
+  int32_t Lq, Lk;
+  int32_t tile, part, parts, pad;
+};
+// 16 rows of a sequence whose parts are merged.
+struct MergeItem {
+  int64_t q0, p0;
+  int32_t Lq, parts, block, pad;
+};
+// A key block's walk over the query tiles from the last one down, or a segment of
+// it: `count` tiles from tile `first` down; fp32 sums to slot `slot` unless < 0.
+struct KeyItem {
+  int64_t q0, k0, r0;      // r0: first row of the sequence among the row terms
+  int32_t Lq, Lk;
+  int32_t kb, first, count, slot;
+};
+// A key block whose segments' sums are added: slots slot .. slot + n - 1.
+struct FoldItem {
+  int64_t k0;
+  int32_t Lk, kb, slot, n;
+};
+// A tile of row terms: query tile `tile` of a sequence.
+struct TermItem {
+  int64_t q0, r0;
+  int32_t Lq, Lk, tile, pad;
+};
+struct DqItem {
+  int64_t q0, k0, r0;
+  int32_t Lq, Lk, tile, pad;
+};
+
+struct PlanHeader {
+  uint64_t magic;
+  int64_t bytes;                       // of the whole plan
+  int64_t total_q, total_k;            // rows up to the end of the last sequence
+  int64_t part_rows;                   // fp32 partial rows of the forward
+  int64_t term_rows;                   // row terms of one key/value head
+  int64_t slots;                       // segment sums of one key/value head
+  int64_t longest_q, longest_k;
+  int32_t n_seq, Hq, Hkv, causal;
+  int32_t fwd_ks, dq_ks;               // key parts inside a workgroup
+  int32_t n_fwd, n_merge, n_key, n_fold, n_term, n_dq;
+  int64_t at_fwd, at_merge, at_key, at_fold, at_term, at_dq;     // byte offsets
+};
+
+// Query tokens of a 128-row tile of the backward.
+__host__ __device__ inline int tile_tokens(int G) { return 128 / G; }
+
+// ---- forward (varlen_fwd.hip) ----------------------------------------------
+struct RowFwdArgs {
+  HeadView q, k, v, o;       // k, v: batch = elements from one cache to the next
+  float* lse;
+  int64_t lse_head;          // elements from one head's log-sum-exps to the next
+  float *part_o, *part_lse;  // fp32 rows of 128, and their log-sum-exps
+  const RowItem* items;      // planned sequences
+  const int32_t* lens;       // caches: valid rows of each
+  int64_t cap;
+  RowItem one;               // a single sequence (the shared prefix)
+  int Hkv, G, causal;
+  int B, nq, splits, part0;  // caches: their first part among those of a row
+};
+enum RowMode { kRowsPlanned = 0, kRowsCache = 1, kRowsOne = 2 };
+// `blocks` items (of every key/value head).
+hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks, hipStream_t st);
+
+struct RowMergeArgs {
+  const float *part_o, *part_lse;
+  HeadView o;
+  float* lse;
+  int64_t lse_head;
+  const MergeItem* items;    // planned sequences; else all rows of B caches
+  int64_t rows;              // B * nq * Hq
+  int Hq, parts, nq;
+};
+hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t blocks, hipStream_t st);
+
+}  // namespace upipe

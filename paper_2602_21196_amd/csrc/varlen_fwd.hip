@@ -1,0 +1,522 @@
+// Attention forward over packed sequences of different lengths, over caches with
+// lengths on the device, and over a prefix that a batch shares, for gfx950.
+//
+//   o_i = sum_j softmax_j(q_i.k_j / sqrt d) v_j,   lse_i = log sum_j exp(q_i.k_j / sqrt d)
+// over the keys that row i sees: with causal, j <= i + Lk - Lq of its own sequence.
+//
+// Work decomposition: as in the forward over equal lengths (128-key stages of K and
+// V rows in LDS, double-buffered; S^T = K Q^T by MFMA, a row's scores in one lane
+// pair, P in registers as the operand of O^T += V^T P^T; one pass with a running
+// reference maximum), with
+//   - rows packed by key/value group (varlen.h), KS parts of every stage's keys by a
+//     workgroup's waves: 256, 128 or 64 rows;
+//   - one launch over a host-made list of tiles, longest first;
+//   - a tile's keys cut into parts where tiles are few: fp32 results, merged.
+#include "varlen.h"
+
+namespace upipe {
+
+namespace {
+
+constexpr int BKS = 128;       // keys per LDS stage
+constexpr int K_TILE = BKS * HEAD_DIM * 2;       // [128][128] bf16 = 32 KB
+constexpr int V_TILE = HEAD_DIM * BKS * 2;       // [128][128] bf16 = 32 KB
+constexpr int STAGE = K_TILE + V_TILE;
+constexpr float kSumMax = 256.f;   // lazy-rescale bound on a lane's stage sum (2^8)
+
+// P of a stage as the bf16 operand of P . V (one rounding of 2^-9 a weight, as the
+// matrix instructions take it), and this lane's sum of it in fp32, before that
+// rounding: lse is good to fp32.
+template <int NT>
+__device__ __forceinline__ float tile_probs(const f32x16 (&st)[NT], bf16x8 (&pf)[NT][2],
+                                            float m_ref, float sl2) {
+  float ls = 0.f;
+#pragma unroll
+  for (int tt = 0; tt < NT; ++tt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const float p0 = fast_exp2(fmaf(st[tt][i], sl2, -m_ref));
+      const float p1 = fast_exp2(fmaf(st[tt][i + 1], sl2, -m_ref));
+      pf[tt][i >> 3][i & 7] = (bf16)p0;
+      pf[tt][i >> 3][(i & 7) + 1] = (bf16)p1;
+      ls += p0 + p1;
+    }
+  return ls;
+}
+
+// One stage (in `buf`) for one wave: the 32 NT keys from key kb on, rows k_part..
+// of the stage.  This lane's row sees the keys up to `lim`, the wave's first row
+// those up to lim_w.  copy_k and copy_v issue the next stage's copies.
+template <int NT, class CopyK, class CopyV>
+__device__ __forceinline__ void fwd_stage(const char* buf, int kb, int k_part, int lane,
+                                          const bf16x8 (&qf)[8], int lim, int lim_w,
+                                          f32x16 (&oacc)[4], float& m_ref, float& l_run,
+                                          const CopyK& copy_k, const CopyV& copy_v) {
+  const float sl2 = 1.4426950408889634f * 0.08838834764831845f;  // log2(e)/sqrt(128)
+  const int r32 = lane & 31, g = lane >> 5;
+  f32x16 st[NT];
+#pragma unroll
+  for (int tt = 0; tt < NT; ++tt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) st[tt][i] = 0.f;
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int tt = 0; tt < NT; ++tt)
+      st[tt] = mfma32x32x16(lds_read_b128(buf, swz256(k_part + 32 * tt + r32, 2 * s + g)),
+                            qf[s], st[tt]);
+  // Keep six K fragment reads in flight ahead of the MFMAs: left alone,
+  // the scheduler reads two, waits for them and multiplies, exposing the
+  // LDS latency every two MFMAs.
+  __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+  for (int i = 0; i < 8 * NT - 6; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
+  // The next stage's copies follow the two blocks of products they can hide
+  // behind: a wave stands still while the CU takes them, and at the top of
+  // the stage nothing of it is under way.  Against there: one head over 4096
+  // keys 43 -> 39 us, 8 heads over 4096 56 -> 52, 4 over 8192 90 -> 86, long
+  // calls, where other waves fill the gap, within 0.5 %.
+  copy_k();
+  // Mask keys past the row's last visible key (wave-uniform test first).
+  if (kb + 32 * NT - 1 > lim_w) {
+#pragma unroll
+    for (int tt = 0; tt < NT; ++tt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = kb + 32 * tt + 8 * (i >> 2) + 4 * g + (i & 3);
+        if (key > lim) st[tt][i] = -INFINITY;
+      }
+  }
+  bf16x8 pf[NT][2];
+  float ls = tile_probs<NT>(st, pf, m_ref, sl2);
+  if (__builtin_amdgcn_ballot_w64(!(ls <= kSumMax)) != 0) {
+    float mx = st[0][0];
+#pragma unroll
+    for (int tt = 0; tt < NT; ++tt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, st[tt][i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32)) * sl2;
+    const float m_new = fmaxf(m_ref, mx);
+    const float alpha = fast_exp2(m_ref - m_new);
+    m_ref = m_new;
+    l_run *= alpha;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) oacc[dt][i] *= alpha;
+    ls = tile_probs<NT>(st, pf, m_ref, sl2);
+  }
+  copy_v();
+  l_run += ls;
+#pragma unroll
+  for (int c = 0; c < 2 * NT; ++c)
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+      oacc[dt] = mfma32x32x16(tr_operand(buf + K_TILE, k_part + 16 * c, 32 * dt, lane),
+                              pf[c >> 1][c & 1], oacc[dt]);
+  // Stream the V^T fragments: four (eight transposing reads) ahead, then
+  // two reads per MFMA (the default schedule issued bursts of eight
+  // reads and waited between them).
+  __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+  for (int i = 0; i < 8 * NT - 4; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+}
+
+// The KS parts of every row folded in fp32, in ascending key order: parts 1..
+// pass (m_ref, l, acc) through the stage buffers (16 KB per wave) with fold_out,
+// part 0 takes them with fold_in; a barrier before each.
+template <int KS>
+__device__ __forceinline__ void fold_out(char* smem, int ks, int wq, int lane,
+                                         const f32x16 (&oacc)[4], float m_ref, float l_tot) {
+  constexpr int NQW = 8 / KS;
+  float* fold = reinterpret_cast<float*>(smem);
+  float* fold_ml = fold + (KS - 1) * NQW * 4096;
+  const int slot = (ks - 1) * NQW + wq;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      f32x4 v;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) v[b] = oacc[dt][4 * a + b];
+      *reinterpret_cast<f32x4*>(fold + slot * 4096 + (4 * dt + a) * 256 + lane * 4) = v;
+    }
+  fold_ml[slot * 128 + lane] = m_ref;
+  fold_ml[slot * 128 + 64 + lane] = l_tot;
+}
+
+template <int KS>
+__device__ __forceinline__ void fold_in(const char* smem, int wq, int lane, f32x16 (&oacc)[4],
+                                        float& m_ref, float& l_tot) {
+  constexpr int NQW = 8 / KS;
+  const float* fold = reinterpret_cast<const float*>(smem);
+  const float* fold_ml = fold + (KS - 1) * NQW * 4096;
+#pragma unroll
+  for (int p = 1; p < KS; ++p) {
+    const int slot = (p - 1) * NQW + wq;
+    const float m_p = fold_ml[slot * 128 + lane], l_p = fold_ml[slot * 128 + 64 + lane];
+    const float m_new = fmaxf(m_ref, m_p);
+    const float a0 = fast_exp2(m_ref - m_new), a1 = fast_exp2(m_p - m_new);
+    m_ref = m_new;
+    l_tot = l_tot * a0 + l_p * a1;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const f32x4 v =
+            *reinterpret_cast<const f32x4*>(fold + slot * 4096 + (4 * dt + a) * 256 + lane * 4);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) oacc[dt][4 * a + b] = oacc[dt][4 * a + b] * a0 + v[b] * a1;
+      }
+  }
+}
+
+
+// Row r of Lq * G against its keys by plain arithmetic, for the rows whose result
+// came out infinite or not a number: a masked key's weight is 0, but the matrix
+// instructions also multiply that 0 by a value that may be neither.  The lane pair
+// of a row has its query and output elements as the tile has them.  Ends early
+// once a visible score is not a number: so is then the whole row.
+__device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const bf16* v, int64_t v_row,
+                                         int64_t key0, int64_t key1, const bf16x8 (&qf)[8], int g,
+                                         f32x16 (&oacc)[4], float& m_ref, float& l) {
+  const float sl2 = 1.4426950408889634f * 0.08838834764831845f;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
+  m_ref = -1e30f;
+  l = 0.f;
+  for (int64_t j = key0; j < key1; ++j) {
+    const bf16* kp = k + j * k_row + 8 * g;
+    float s = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const bf16x8 kk = *reinterpret_cast<const bf16x8*>(kp + 16 * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s = fmaf((float)kk[e], (float)qf[c][e], s);
+    }
+    s = (s + __shfl_xor(s, 32)) * sl2;
+    const float m_new = fmaxf(m_ref, s), alpha = fast_exp2(m_ref - m_new);
+    const float p = fast_exp2(s - m_new);
+    m_ref = m_new;
+    l = l * alpha + p;
+    const bf16* vp = v + j * v_row + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const bf16x4 vv = *reinterpret_cast<const bf16x4*>(vp + 32 * dt + 8 * a);
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+          oacc[dt][4 * a + b] = fmaf(p, (float)vv[b], oacc[dt][4 * a + b] * alpha);
+      }
+    if (!(p == p) || !(l == l)) {
+      l = NAN;
+      break;
+    }
+  }
+}
+
+// A workgroup: BQ packed rows of one key/value head against a range of its keys.
+template <int KS, int MODE>
+__global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
+  constexpr int NQW = 8 / KS;            // waves along the rows
+  constexpr int NT = 4 / KS;             // 32-key tiles of a stage per wave
+  constexpr int BQ = 32 * NQW;           // rows per workgroup
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int t = threadIdx.x;
+  const int lane = t & 63;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wq = KS == 1 ? w : w % NQW, ks = KS == 1 ? 0 : w / NQW;
+  const int r32 = lane & 31, g = lane >> 5;
+  const int kvh = blockIdx.x % a.Hkv, idx = blockIdx.x / a.Hkv, G = a.G, Hq = a.Hkv * G;
+
+  RowItem it;
+  int64_t cache = 0, lse_at, part_rows;
+  if (MODE == kRowsPlanned) {
+    it = a.items[idx];
+    lse_at = it.q0;
+    part_rows = (int64_t)it.Lq * Hq;
+  } else if (MODE == kRowsOne) {
+    it = a.one;
+    it.part = idx % it.parts;
+    it.tile = idx / it.parts;
+    lse_at = 0;                  // always parts
+    part_rows = (int64_t)it.Lq * Hq;
+  } else {
+    const int tiles = (a.nq * G + BQ - 1) / BQ, b = idx / a.splits % a.B;
+    it.tile = idx / a.splits / a.B % tiles;
+    it.part = idx % a.splits + a.part0;
+    it.parts = a.splits;
+    it.q0 = (int64_t)b * a.nq;
+    it.k0 = 0;
+    it.p0 = it.q0 * Hq;
+    it.Lq = a.nq;
+    it.Lk = (int)min(max((int64_t)a.lens[b], (int64_t)0), a.cap);
+    cache = b;
+    lse_at = it.q0 * Hq;
+    part_rows = (int64_t)a.B * a.nq * Hq;
+  }
+  const int n_rows = it.Lq * G, delta = it.Lk - it.Lq;
+  const int r0 = it.tile * BQ, rw = r0 + 32 * wq, row = rw + r32;
+  const bool row_ok = row < n_rows;
+  const int tok = row / G, hg = row - tok * G;
+
+  const uint32_t kb_row = (uint32_t)(a.k.row * 2), vb_row = (uint32_t)(a.v.row * 2);
+  const bf16* kp = a.k.p + cache * a.k.batch + it.k0 * a.k.row + kvh * a.k.head;
+  const bf16* vp = a.v.p + cache * a.v.batch + it.k0 * a.v.row + kvh * a.v.head;
+  uint32_t offk[4], offv[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * (4 * w + i) + (lane >> 4);       // stage row, 16 lanes per row
+    offk[i] = r * kb_row + ((uint32_t)((lane & 15) ^ (r & 15)) << 4);
+    offv[i] = r * vb_row + (((lane & 15) ^ tsw(r)) << 4);
+  }
+
+  // Keys that the workgroup's and this wave's last row, this lane's row and the
+  // wave's first row see; -1: none.
+  auto last_key = [&](int tk) { return a.causal ? min(tk + delta, it.Lk - 1) : it.Lk - 1; };
+  const int seen = last_key((min(r0 + BQ, n_rows) - 1) / G) + 1;
+  const int nst = max(0, (seen + BKS - 1) / BKS);
+  int j0 = 0, j1 = nst;
+  if (MODE != kRowsPlanned || it.parts > 1) {
+    const int per = (nst + it.parts - 1) / it.parts;
+    j0 = min(nst, per * (MODE == kRowsCache ? it.part - a.part0 : it.part));
+    j1 = min(nst, j0 + per);
+  }
+  const int k_part = 32 * NT * ks;          // first key of this wave's part of a stage
+  const int seen_w = last_key((min(rw + 32, n_rows) - 1) / G) + 1;
+  const int nw = rw >= n_rows ? 0 : max(0, min(j1, (seen_w - k_part + BKS - 1) / BKS));
+  const int lim = last_key(tok), lim_w = last_key(rw / G);
+  const uint32_t lds0 = lds_address(smem);
+  // A stage's rows: 64-bit bases, so a cache may be of any length; rows past the
+  // last key, and those of no stage, read as zero.
+  auto source = [&](const bf16* p, int64_t row_elems, int j) {
+    const int n = j < j1 ? min(BKS, it.Lk - j * BKS) : 0;
+    return rsrc_words(p + (int64_t)j * BKS * row_elems,
+                      n > 0 ? (uint32_t)((n - 1) * (int)row_elems + HEAD_DIM) * 2 : 0);
+  };
+  if (j0 < j1) {
+    copy4_b128(source(kp, a.k.row, j0), offk, 0, lds0 + (j0 & 1) * STAGE + 4096 * w);
+    copy4_b128(source(vp, a.v.row, j0), offv, 0, lds0 + (j0 & 1) * STAGE + K_TILE + 4096 * w);
+  }
+
+  // Q^T B-operand fragments for the whole key loop: lane = row, k-group g covers
+  // head-dim [16s + 8g, 16s + 8g + 8).
+  bf16x8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qf[s][e] = (bf16)0.f;
+  if (row_ok) {
+    const bf16* qp = a.q.p + (it.q0 + tok) * a.q.row + (kvh * G + hg) * a.q.head + 8 * g;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s);
+  }
+
+  f32x16 oacc[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
+  // Reference max of the scaled scores (log2 domain): a finite stand-in for
+  // -inf, so that a stage whose keys are all masked for a row leaves it at
+  // p = 0 rather than producing 0 * inf.
+  float m_ref = -1e30f;
+  float l_run = 0.f;         // this lane's partial row sum
+
+  for (int j = j0; j < j1; ++j) {
+    const char* buf = smem + (j & 1) * STAGE;
+    wait_vmem();
+    __syncthreads();   // stage j landed for all waves; stage j-1's buffer is free
+    const uint32_t nlds = lds0 + ((j + 1) & 1) * STAGE + 4096 * w;
+    const i32x4 nk = source(kp, a.k.row, j + 1), nv = source(vp, a.v.row, j + 1);
+    if (j >= nw) {                          // whole stage masked for this wave
+      copy4_b128(nk, offk, 0, nlds);
+      copy4_b128(nv, offv, 0, nlds + K_TILE);
+      continue;
+    }
+    fwd_stage<NT>(buf, j * BKS + k_part, k_part, lane, qf, lim, lim_w, oacc, m_ref, l_run,
+                  [&]() { copy4_b128(nk, offk, 0, nlds); },
+                  [&]() { copy4_b128(nv, offv, 0, nlds + K_TILE); });
+  }
+
+  wait_vmem();       // the last stage's empty copies (to LDS) have ended
+  float l_tot = l_run + __shfl_xor(l_run, 32);
+  if (KS > 1) {
+    __syncthreads();   // every wave is done reading the last stage, and copying
+    if (ks > 0) fold_out<KS>(smem, ks, wq, lane, oacc, m_ref, l_tot);
+    __syncthreads();
+    if (ks > 0) return;
+    fold_in<KS>(smem, wq, lane, oacc, m_ref, l_tot);
+  }
+  // A masked value that is infinite or not a number leaves NaN in the rows of its
+  // stage: those are formed again without it.
+  {
+    float z = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z = fmaf(oacc[dt][i], 0.f, z);
+    z += __shfl_xor(z, 32);
+    if (row_ok && !(z == z)) {      // both lanes of a row
+      const int64_t key1 = min((int64_t)lim + 1, (int64_t)j1 * BKS);
+      careful_row(kp, a.k.row, vp, a.v.row, (int64_t)j0 * BKS, key1, qf, g, oacc, m_ref, l_tot);
+    }
+  }
+  if (!row_ok) return;
+  const bool some = !(l_tot <= 0.f);
+  const float inv = some ? 1.f / l_tot : 0.f;   // no visible key: O = 0
+  const float row_lse = some ? (m_ref + __log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+  const int h = kvh * G + hg;
+  if (MODE != kRowsPlanned || it.parts > 1) {
+    const int64_t at = it.p0 + it.part * part_rows + (int64_t)tok * Hq + h;
+    if (g == 0) a.part_lse[at] = row_lse;
+    if (!some) return;           // the merge does not read the row of an empty part
+    float* pp = a.part_o + at * HEAD_DIM + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 ov;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) ov[b] = oacc[dt][4 * i + b] * inv;
+        *reinterpret_cast<f32x4*>(pp + 32 * dt + 8 * i) = ov;
+      }
+    return;
+  }
+  bf16* op = a.o.p + (it.q0 + tok) * a.o.row + h * a.o.head + 4 * g;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x4 ov;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) ov[b] = (bf16)(oacc[dt][4 * i + b] * inv);
+      *reinterpret_cast<bf16x4*>(op + 32 * dt + 8 * i) = ov;
+    }
+  if (g == 0) a.lse[lse_at + h * a.lse_head + tok] = row_lse;
+}
+
+// The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
+// rounding.  Sixteen lanes a row, GP groups of them to share many parts.
+template <int GP, bool PLANNED>
+__global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
+  __shared__ float sh[GP > 1 ? GP : 1][HEAD_DIM + 2];
+  const int c = threadIdx.x & 15, grp = threadIdx.x >> 4;
+  const int gp = GP > 1 ? grp : 0;
+  int64_t r, q0 = 0, p0 = 0, rows = a.rows;
+  int parts = a.parts;
+  if (PLANNED) {
+    const MergeItem it = a.items[blockIdx.x];
+    q0 = it.q0;
+    p0 = it.p0;
+    rows = (int64_t)it.Lq * a.Hq;
+    parts = it.parts;
+    r = (int64_t)it.block * 16 + grp;
+  } else {
+    r = (int64_t)blockIdx.x * (16 / GP) + (GP > 1 ? 0 : grp);
+  }
+  if (r >= rows) return;         // GP > 1: a whole workgroup
+  const float* pl = a.part_lse + p0 + r;
+  float m = -INFINITY;
+  for (int i = gp; i < parts; i += GP) m = fmaxf(m, pl[i * rows]);
+  // (a NaN is passed over by fmaxf and comes in with its weight)
+  float l = 0.f, acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+  const float* po = a.part_o + (p0 + r) * HEAD_DIM + 8 * c;
+#pragma unroll 4
+  for (int i = gp; i < parts; i += GP) {
+    const float li = pl[i * rows];
+    if (li == -INFINITY) continue;       // an empty part: its row is not written
+    const float wt = li == m ? 1.f : __expf(li - m);
+    const float* p = po + i * rows * HEAD_DIM;
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+    l += wt;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc[e] = fmaf(wt, lo[e], acc[e]);
+      acc[4 + e] = fmaf(wt, hi[e], acc[4 + e]);
+    }
+  }
+  if (GP > 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sh[gp][8 * c + e] = acc[e];
+    if (c == 0) {
+      sh[gp][HEAD_DIM] = m;
+      sh[gp][HEAD_DIM + 1] = l;
+    }
+    __syncthreads();
+    if (gp > 0) return;
+    float mm = m;
+    for (int i = 1; i < GP; ++i) mm = fmaxf(mm, sh[i][HEAD_DIM]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    for (int i = 0; i < GP; ++i) {
+      const float mi = sh[i][HEAD_DIM], ln = sh[i][HEAD_DIM + 1];
+      if (mi == -INFINITY && ln == 0.f) continue;
+      const float wt = mi == mm ? 1.f : __expf(mi - mm);
+      l = fmaf(wt, ln, l);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = fmaf(wt, sh[i][8 * c + e], acc[e]);
+    }
+    m = mm;
+  }
+  const bool some = !(l <= 0.f);
+  const int64_t tok = r / a.Hq;
+  const int h = (int)(r - tok * a.Hq);
+  bf16x8 out;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) out[e] = (bf16)(some ? acc[e] / l : 0.f);
+  *reinterpret_cast<bf16x8*>(a.o.p + (q0 + tok) * a.o.row + h * a.o.head + 8 * c) = out;
+  if (c == 0) {
+    const float v = some ? fmaf(__log2f(l), 0.6931471805599453f, m) : -INFINITY;
+    if (PLANNED) a.lse[q0 + tok + h * a.lse_head] = v;
+    else a.lse[((tok / a.nq) * a.Hq + h) * a.nq + tok % a.nq] = v;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
+  const dim3 grid((unsigned)(blocks * a.Hkv));
+#define UPIPE_ROWS(K, M) hipLaunchKernelGGL((rows_fwd_kernel<K, M>), grid, dim3(512), 0, st, a)
+  if (mode == kRowsPlanned) {
+    if (ks == 1) UPIPE_ROWS(1, kRowsPlanned);
+    else if (ks == 2) UPIPE_ROWS(2, kRowsPlanned);
+    else UPIPE_ROWS(4, kRowsPlanned);
+  } else if (mode == kRowsOne) {
+    if (ks == 1) UPIPE_ROWS(1, kRowsOne);
+    else if (ks == 2) UPIPE_ROWS(2, kRowsOne);
+    else UPIPE_ROWS(4, kRowsOne);
+  } else {
+    UPIPE_ROWS(4, kRowsCache);
+  }
+#undef UPIPE_ROWS
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t blocks, hipStream_t st) {
+  if (a.items != nullptr) {
+    hipLaunchKernelGGL((rows_merge_kernel<1, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  } else if (a.parts > 16) {
+    hipLaunchKernelGGL((rows_merge_kernel<16, false>), dim3((unsigned)a.rows), dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((rows_merge_kernel<1, false>), dim3((unsigned)((a.rows + 15) / 16)), dim3(256),
+                       0, st, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace upipe

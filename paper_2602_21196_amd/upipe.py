@@ -81,6 +81,16 @@ _SIGNATURES = {
                                   _c_void_p, _size, _c_void_p]),
     "upipe_gemm_bf16": (_int, [_c_void_p, _c_void_p, _c_void_p, _i64, _i64, _i64,
                                _c_void_p]),
+    "upipe_varlen_plan_size": (_size, [_c_void_p, _c_void_p, _int, _int, _int, _int, _int]),
+    "upipe_varlen_plan": (_int, [_c_void_p, _c_void_p, _int, _int, _int, _int, _int, _c_void_p,
+                                 _size]),
+    "upipe_attn_fwd_varlen_workspace_size": (_size, [_c_void_p]),
+    "upipe_attn_fwd_varlen": (_int, [upipe_heads] * 4 + [_fptr, _i64, _c_void_p, _c_void_p,
+                                                         _c_void_p, _size, _c_void_p]),
+    "upipe_attn_decode_workspace_size": (_size, [_i64, _int, _i64, _i64, _int, _int, _int]),
+    "upipe_attn_decode": (_int, [upipe_heads, upipe_heads, _i64, upipe_heads, _i64, _c_void_p,
+                                 upipe_heads, upipe_heads, upipe_heads, _fptr, _i64, _int, _i64,
+                                 _i64, _int, _int, _int, _c_void_p, _size, _c_void_p]),
     "upipe_qk_norm_rope": (_int, [upipe_heads, upipe_heads, _c_void_p, _c_void_p, _int,
                                   _c_void_p, upipe_heads, upipe_heads, _i64, _int, _int, _int,
                                   _dbl, _dbl, _c_void_p]),
@@ -241,6 +251,33 @@ def upipe_layer_bwd_ex(x, wqkv, wo, o_saved, lse_saved, dy, dx, dwqkv, dwo, B, S
 
 def upipe_gemm_bf16(a, b, c, M, N, K, stream):
     return lib().upipe_gemm_bf16(a, b, c, M, N, K, stream)
+
+
+def upipe_varlen_plan_size(cu_q, cu_k, n_seq, Hq, Hkv, d, causal):
+    return lib().upipe_varlen_plan_size(cu_q, cu_k, n_seq, Hq, Hkv, d, causal)
+
+
+def upipe_varlen_plan(cu_q, cu_k, n_seq, Hq, Hkv, d, causal, plan, plan_bytes):
+    return lib().upipe_varlen_plan(cu_q, cu_k, n_seq, Hq, Hkv, d, causal, plan, plan_bytes)
+
+
+def upipe_attn_fwd_varlen_workspace_size(plan):
+    return lib().upipe_attn_fwd_varlen_workspace_size(plan)
+
+
+def upipe_attn_fwd_varlen(q, k, v, o, lse, lse_head, plan, plan_dev, ws, ws_bytes, stream):
+    return lib().upipe_attn_fwd_varlen(q, k, v, o, lse, lse_head, plan, plan_dev, ws, ws_bytes,
+                                       stream)
+
+
+def upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d):
+    return lib().upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d)
+
+
+def upipe_attn_decode(q, k, k_cache, v, v_cache, lens, k_prefix, v_prefix, o, lse, B, nq, cap, P,
+                      Hq, Hkv, d, ws, ws_bytes, stream):
+    return lib().upipe_attn_decode(q, k, k_cache, v, v_cache, lens, k_prefix, v_prefix, o, lse, B,
+                                   nq, cap, P, Hq, Hkv, d, ws, ws_bytes, stream)
 
 
 def upipe_qk_norm_rope(q, k, wq, wk, w_fp32, positions, q_out, k_out, T, Hq, Hkv, d, base, eps,
@@ -678,3 +715,144 @@ def qk_norm_rope_bwd(q, k, wq, wk, positions, base, dq_out, dk_out, eps=1e-6, ou
                                     float(base), float(eps), ws.data_ptr(), ws.numel(), stream)
     _check("upipe_qk_norm_rope_bwd", st)
     return dq, dk, dwq, dwk
+
+
+# --------------------------------------- packed sequences, caches, prefixes
+
+def _offsets(cu, name):
+    """A host list of offsets as a C array of int64."""
+    torch = _torch()
+    if isinstance(cu, torch.Tensor):
+        if cu.is_cuda:
+            raise ValueError(f"{name} is planned on the host: pass a list or a CPU tensor")
+        cu = cu.tolist()
+    cu = [int(x) for x in cu]
+    if not cu:
+        raise ValueError(f"{name} needs n + 1 offsets")
+    return (_i64 * len(cu))(*cu), cu
+
+
+class VarlenPlan:
+    """The work of one batch of packed sequences: sequence s has the queries
+    cu_q[s] .. cu_q[s+1] and the keys cu_k[s] .. cu_k[s+1] (the same, unless given).
+    Host offsets, 0 first.  Made once per batch, for all layers, forward and backward."""
+
+    def __init__(self, cu_q, cu_k=None, *, Hq, Hkv, causal=True, device="cuda"):
+        torch = _torch()
+        c_q, cu_q = _offsets(cu_q, "cu_q")
+        c_k, cu_k = (c_q, cu_q) if cu_k is None else _offsets(cu_k, "cu_k")
+        if len(cu_q) != len(cu_k):
+            raise ValueError(f"cu_q has {len(cu_q)} offsets, cu_k {len(cu_k)}")
+        args = (c_q, c_k, len(cu_q) - 1, int(Hq), int(Hkv), 128, int(bool(causal)))
+        need = upipe_varlen_plan_size(*args)
+        if need == 0:
+            raise UpipeError("upipe_varlen_plan_size", -1)
+        self._host = bytearray(need)
+        self._buf = (ctypes.c_char * need).from_buffer(self._host)
+        self.host = ctypes.addressof(self._buf)
+        _check("upipe_varlen_plan", upipe_varlen_plan(*args, self.host, need))
+        self.Hq, self.Hkv, self.causal = int(Hq), int(Hkv), bool(causal)
+        self.total_q, self.total_k = cu_q[-1], cu_k[-1]
+        self.fwd_workspace = upipe_attn_fwd_varlen_workspace_size(self.host)
+        self.dev = torch.frombuffer(self._host, dtype=torch.uint8).to(device)
+
+
+def _packed(t, name, rows, H):
+    """upipe_heads of [>= rows, H, 128]."""
+    v = _rows(t, name)
+    if t.shape[0] < rows or t.shape[1] != H or t.shape[2] != 128:
+        raise ValueError(f"{name} must be [T,{H},128] with T >= {rows}, got {tuple(t.shape)}")
+    return v
+
+
+def _packed_lse(lse, q, plan):
+    T = q.shape[0]
+    if lse.dim() != 2 or lse.shape[0] != plan.Hq or lse.shape[1] < T:
+        raise ValueError(f"lse must be [{plan.Hq},{T}], got {tuple(lse.shape)}")
+    return _ptr(lse, _torch().float32, "lse"), lse.shape[1]
+
+
+def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
+    """(o [T,Hq,d] bf16, lse [Hq,T] fp32) of the packed q [T,Hq,d], k, v [Tk,Hkv,d]
+    (strided views with dense rows) of a VarlenPlan.  Rows behind the last sequence
+    are left as they are in out = (o, lse), 0 and -inf in new tensors."""
+    torch = _torch()
+    Tq, Tk = plan.total_q, plan.total_k
+    views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
+             _packed(v, "v", Tk, plan.Hkv))
+    if out is None:
+        o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        lse = torch.empty((plan.Hq, q.shape[0]), dtype=torch.float32, device=q.device)
+        if Tq < q.shape[0]:
+            o[Tq:] = 0
+            lse[:, Tq:] = float("-inf")
+    else:
+        o, lse = out
+    ws = _workspace(ws, plan.fwd_workspace, q.device, "upipe_attn_fwd_varlen_workspace_size")
+    with _Call(q=q, k=k, v=v, o=o, lse=lse, plan=plan.dev, ws=ws) as stream:
+        st = upipe_attn_fwd_varlen(*views, _packed(o, "o", Tq, plan.Hq), *_packed_lse(lse, q, plan),
+                                   plan.host, plan.dev.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    _check("upipe_attn_fwd_varlen", st)
+    return o, lse
+
+
+def _cache(t, name, B, Hkv):
+    """(upipe_heads of one cache, elements from one to the next) of [B, cap, Hkv, d]."""
+    if not isinstance(t, _torch().Tensor) or t.dim() != 4:
+        raise ValueError(f"{name} must be [B,cap,Hkv,d]")
+    _shape(t, (B, t.shape[1], Hkv, 128), name)
+    v = _rows(t[0], name)
+    return v, t.stride(0) if B > 1 else 0
+
+
+def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=None, ws=None):
+    """(o like q, lse [B,Hq,nq] fp32) of the new tokens q [B,nq,Hq,d] against the caches
+    [B,cap,Hkv,d], of which lens [B] (int32, on the device) rows are valid, the new tokens'
+    own among them, behind the rows [P,Hkv,d] of a prefix that all share, if given."""
+    torch = _torch()
+    if q.dim() != 4:
+        raise ValueError(f"q must be [B,nq,Hq,d], got {tuple(q.shape)}")
+    if k_cache.dim() != 4 or tuple(k_cache.shape) != tuple(v_cache.shape):
+        raise ValueError("k_cache and v_cache must be [B,cap,Hkv,d], got "
+                         f"{tuple(k_cache.shape)}, {tuple(v_cache.shape)}")
+    if (k_prefix is None) != (v_prefix is None):
+        raise ValueError("attn_decode: pass both k_prefix and v_prefix, or neither")
+    B, nq, Hq, d = q.shape
+    cap, Hkv = k_cache.shape[1:3]
+    if B < 1 or cap < 1:
+        raise ValueError(f"attn_decode: no sequences or no cache rows ({B}, {cap})")
+    _shape(lens, (B,), "lens")
+    vq = _rows(_flat_tokens(q, "q"), "q")
+    vk, k_step = _cache(k_cache, "k_cache", B, Hkv)
+    vv, v_step = _cache(v_cache, "v_cache", B, Hkv)
+    P, none = 0, upipe_heads(None, 0, 0)
+    vkp = vvp = none
+    if k_prefix is not None:
+        P = k_prefix.shape[0]
+        vkp = _rows(k_prefix, "k_prefix", (P, Hkv, d))
+        vvp = _rows(v_prefix, "v_prefix", (P, Hkv, d))
+    if out is None:
+        o = torch.empty((B, nq, Hq, d), dtype=torch.bfloat16, device=q.device)
+        lse = torch.empty((B, Hq, nq), dtype=torch.float32, device=q.device)
+    else:
+        o, lse = out
+        _shape(o, q.shape, "o")
+        _shape(lse, (B, Hq, nq), "lse")
+    need = upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d)
+    ws = _workspace(ws, need, q.device, "upipe_attn_decode_workspace_size")
+    with _Call(q=q, k_cache=k_cache, v_cache=v_cache, lens=lens, k_prefix=k_prefix,
+               v_prefix=v_prefix, o=o, lse=lse, ws=ws) as stream:
+        st = upipe_attn_decode(vq, vk, k_step, vv, v_step, _ptr(lens, torch.int32, "lens"), vkp, vvp,
+                               _rows(_flat_tokens(o, "o"), "o"), _ptr(lse, torch.float32, "lse"),
+                               B, nq, cap, P, Hq, Hkv, d, ws.data_ptr(), ws.numel(), stream)
+    _check("upipe_attn_decode", st)
+    return o, lse
+
+
+def _flat_tokens(t, name):
+    """[B, nq, H, d] as [B nq, H, d], without a copy."""
+    try:
+        return t.view(t.shape[0] * t.shape[1], *t.shape[2:])
+    except RuntimeError:
+        raise ValueError(f"{name}: the tokens of all sequences must be evenly spaced, got "
+                         f"strides {t.stride()}") from None
