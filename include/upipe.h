@@ -319,6 +319,23 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
                           int64_t lse_head, const void* plan, const void* plan_dev, void* ws,
                           size_t ws_bytes, hipStream_t stream);
 
+/* The gradients of attention over packed sequences, with the forward's plan:
+ *   q, k, v, o, lse   as given to and left by upipe_attn_fwd_varlen
+ *   dout              upstream gradient of o, rows [.., Hq, d]
+ *   dq, dk, dv        out: rows [.., Hq, d], [.., Hkv, d] (summed over each group's
+ *                     query heads); dq may be q or dout.  They may be columns of one
+ *                     buffer, as q, k, v of a projection are.
+ * Rows of 128 / G tokens (G = Hq / Hkv) of q and of dout, all heads of a group, must
+ * span less than 2^30 bytes (UPIPE_ERR_UNSUPPORTED).  P and dS are rounded to bf16 for
+ * their products, every sum is fp32 in a fixed order.  A masked pair's infinite or NaN
+ * row of q, k or dout may reach the gradients of rows within 128 of it in its
+ * sequence. */
+size_t upipe_attn_bwd_varlen_workspace_size(const void* plan);
+int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_heads o,
+                          const float* lse, int64_t lse_head, upipe_heads dout, upipe_heads dq,
+                          upipe_heads dk, upipe_heads dv, const void* plan, const void* plan_dev,
+                          void* ws, size_t ws_bytes, hipStream_t stream);
+
 /* ------------------------------------------------------------------------
  * Attention of a few new tokens of every sequence against its cache, and against
  * a prefix that all sequences share.

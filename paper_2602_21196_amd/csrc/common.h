@@ -96,6 +96,19 @@ __device__ __forceinline__ void copy2x2_b128(i32x4 r0, i32x4 r1, uint32_t voff0,
       :: "s"(lds), "v"(voff0), "v"(voff1), "s"(r0), "s"(r1), "s"(soff), "n"(GAP - 1024)
       : "scc");
 }
+// The same with offsets of its own for each source.
+template <int GAP>
+__device__ __forceinline__ void copy2x2_b128(i32x4 r0, i32x4 r1, uint32_t voff00, uint32_t voff01,
+                                             uint32_t voff10, uint32_t voff11, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %5, 0 offen lds\n\t"
+      "s_add_u32 m0, m0, %7\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %6, 0 offen lds\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %6, 0 offen lds"
+      :: "s"(lds), "v"(voff00), "v"(voff01), "v"(voff10), "v"(voff11), "s"(r0), "s"(r1),
+         "n"(GAP - 1024)
+      : "scc");
+}
 __device__ __forceinline__ uint32_t lds_address(const char* p) {
   typedef __attribute__((address_space(3))) const char lds_char;
   return (uint32_t)(uintptr_t)(lds_char*)p;

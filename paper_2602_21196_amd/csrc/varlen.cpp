@@ -149,6 +149,137 @@ FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causa
   return best;
 }
 
+// us of a dK/dV tile of 128 rows, of a workgroup besides its tiles, of the fold's
+// launch and of a segment's sums in it.
+constexpr double kKeyTile = 4.0, kKeyFixed = 8.0, kFoldFixed = 5.0, kFoldSum = 0.065;
+constexpr int64_t kMaxSums = 2048;     // segment sums of all heads: 256 MB of workspace
+
+// Tiles of packed rows that see a key block: first .. last (none: first > last).
+void key_walk(const Lengths& s, int tpt, int kb, int causal, int* first, int* last) {
+  *last = (s.Lq + tpt - 1) / tpt - 1;
+  const int64_t tok = causal ? std::max<int64_t>(0, (int64_t)kb * 128 - (s.Lk - s.Lq)) : 0;
+  *first = (int)std::min<int64_t>(tok / tpt, *last + 1);
+}
+
+// Segments of a walk of n tiles, none longer than `most`, as even as they come.
+int walk_segments(int n, int most) { return n <= most ? 1 : (n + most - 1) / most; }
+
+void key_work(const std::vector<Lengths>& seqs, int G, int causal, int most,
+              std::vector<KeyItem>* keys, std::vector<FoldItem>* folds, int64_t* slots) {
+  const int tpt = tile_tokens(G);
+  keys->clear();
+  folds->clear();
+  *slots = 0;
+  int64_t r0 = 0;
+  for (const Lengths& s : seqs) {
+    const int nkb = (s.Lk + 127) / 128;
+    for (int kb = 0; kb < nkb; ++kb) {
+      int first, last;
+      key_walk(s, tpt, kb, causal, &first, &last);
+      const int n = last - first + 1, segs = walk_segments(n, most);
+      KeyItem it{};
+      it.q0 = s.q0;
+      it.k0 = s.k0;
+      it.r0 = r0;
+      it.Lq = s.Lq;
+      it.Lk = s.Lk;
+      it.kb = kb;
+      for (int i = 0, done = 0; i < segs; ++i) {
+        const int upto = (int)((int64_t)n * (i + 1) / segs);
+        it.first = last - done;
+        it.count = upto - done;
+        it.slot = segs > 1 ? (int32_t)(*slots + i) : -1;
+        keys->push_back(it);
+        done = upto;
+      }
+      if (segs > 1) {
+        folds->push_back({s.k0, s.Lk, kb, (int32_t)*slots, segs});
+        *slots += segs;
+      }
+    }
+    r0 += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
+  }
+  std::stable_sort(keys->begin(), keys->end(),
+                   [](const KeyItem& a, const KeyItem& b) { return a.count > b.count; });
+}
+
+// The longest segment with which all of them are expected to end first.  Many key
+// blocks need no look.
+int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
+  const int tpt = tile_tokens(G), whole = 1 << 30;
+  int64_t blocks = 0;
+  int longest = 1;
+  for (const Lengths& s : seqs) {
+    blocks += (s.Lk + 127) / 128;
+    if (s.Lk > 0) longest = std::max(longest, (s.Lq + tpt - 1) / tpt);
+  }
+  if (blocks * Hkv > 32 * kCUs) return whole;
+  std::vector<KeyItem> keys;
+  std::vector<FoldItem> folds;
+  std::vector<float> cost;
+  int64_t slots;
+  int best = whole;
+  double best_est = 0.0;
+  for (int n : {1, 2, 3, 4, 5, 6, 8, 10, 12, 16}) {
+    const int most = (longest + n - 1) / n;
+    key_work(seqs, G, causal, most, &keys, &folds, &slots);
+    if (n > 1 && slots * Hkv > kMaxSums) continue;
+    cost.clear();
+    for (const KeyItem& k : keys) cost.push_back((float)(kKeyFixed + k.count * kKeyTile));
+    const double est =
+        makespan(cost, Hkv) + (slots > 0 ? kFoldFixed + kFoldSum * slots * Hkv : 0.0);
+    if (n == 1 || est < best_est) {
+      best = most;
+      best_est = est;
+    }
+    if (most <= 2) break;
+  }
+  return best;
+}
+
+// us of a dQ stage with 1 (64 keys), 2 and 4 (128 keys) key parts on a full chip.
+constexpr double kDqStage[3] = {2.5, 2.8, 1.6}, kDqFixed = 4.0;
+
+struct DqWork {
+  DqItem item;
+  int stages;
+};
+
+void dq_work(const std::vector<Lengths>& seqs, int G, int causal, int ks, std::vector<DqWork>* out) {
+  const int rows = 256 / ks, tpt = tile_tokens(G);
+  out->clear();
+  int64_t r0 = 0;
+  for (const Lengths& s : seqs) {
+    for (int t = row_tiles(s.Lq, G, rows) - 1; t >= 0; --t)
+      out->push_back({{s.q0, s.k0, r0, s.Lq, s.Lk, t, 0},
+                      tile_stages(s, G, rows, t, causal) * (ks == 1 ? 2 : 1)});
+    r0 += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
+  }
+  std::stable_sort(out->begin(), out->end(),
+                   [](const DqWork& a, const DqWork& b) { return a.stages > b.stages; });
+}
+
+int choose_dq(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
+  int64_t tiles = 0;
+  for (const Lengths& s : seqs) tiles += row_tiles(s.Lq, G, 256);
+  if (tiles * Hkv >= 16 * kCUs) return 1;
+  std::vector<DqWork> work;
+  std::vector<float> cost;
+  int best = 1;
+  double best_est = 0.0;
+  for (int i = 0; i < 3; ++i) {
+    dq_work(seqs, G, causal, kFwdParts[i], &work);
+    cost.clear();
+    for (const DqWork& w : work) cost.push_back((float)(kDqFixed + w.stages * kDqStage[i]));
+    const double est = makespan(cost, Hkv);
+    if (i == 0 || est < best_est) {
+      best = kFwdParts[i];
+      best_est = est;
+    }
+  }
+  return best;
+}
+
 int check_lengths(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, int d, int causal,
                   std::vector<Lengths>* seqs) {
   if (n < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || !cu_q || !cu_k || (causal != 0 && causal != 1))
@@ -170,6 +301,10 @@ struct Plan {
   PlanHeader h{};
   std::vector<RowItem> fwd;
   std::vector<MergeItem> merge;
+  std::vector<TermItem> terms;
+  std::vector<KeyItem> keys;
+  std::vector<FoldItem> folds;
+  std::vector<DqItem> dqs;
 };
 
 template <class T>
@@ -218,11 +353,33 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
     p->fwd.push_back(w.item);
   }
 
+  const int tpt = tile_tokens(G);
+  for (const Lengths& s : seqs) {
+    for (int t = 0; t < (s.Lq + tpt - 1) / tpt; ++t)
+      p->terms.push_back({s.q0, h.term_rows, s.Lq, s.Lk, t, 0});
+    h.term_rows += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
+  }
+  key_work(seqs, G, causal, choose_segment(seqs, G, Hkv, causal), &p->keys, &p->folds, &h.slots);
+  h.dq_ks = choose_dq(seqs, G, Hkv, causal);
+  std::vector<DqWork> dqs;
+  dq_work(seqs, G, causal, h.dq_ks, &dqs);
+  for (const DqWork& w : dqs) p->dqs.push_back(w.item);
+
+  for (size_t n : {p->terms.size(), p->keys.size(), p->dqs.size(), p->folds.size() * 16})
+    if ((int64_t)n * Hkv > kMaxGrid) return UPIPE_ERR_UNSUPPORTED;
   if ((int64_t)p->fwd.size() * Hkv > kMaxGrid || (int64_t)p->merge.size() > kMaxGrid)
     return UPIPE_ERR_UNSUPPORTED;
   h.n_fwd = (int32_t)p->fwd.size();
   h.n_merge = (int32_t)p->merge.size();
+  h.n_term = (int32_t)p->terms.size();
+  h.n_key = (int32_t)p->keys.size();
+  h.n_fold = (int32_t)p->folds.size();
+  h.n_dq = (int32_t)p->dqs.size();
   int64_t end = round_up(sizeof(PlanHeader), 64);
+  h.at_term = place(&end, p->terms);
+  h.at_key = place(&end, p->keys);
+  h.at_fold = place(&end, p->folds);
+  h.at_dq = place(&end, p->dqs);
   h.at_fwd = place(&end, p->fwd);
   h.at_merge = place(&end, p->merge);
   h.bytes = end;
@@ -242,6 +399,21 @@ const PlanHeader* header_of(const void* plan) {
 size_t parts_bytes(int64_t rows) { return (size_t)rows * (HEAD_DIM + 1) * 4; }
 
 size_t fwd_ws(const PlanHeader& h) { return parts_bytes(h.part_rows) + 16; }
+
+size_t sums_at(const PlanHeader& h) {        // D and lse_c before them
+  return (size_t)round_up(2 * h.Hkv * h.term_rows * 4, 256);
+}
+
+size_t bwd_ws(const PlanHeader& h) {
+  return sums_at(h) + (size_t)h.Hkv * h.slots * 2 * 128 * HEAD_DIM * 4 + 16;
+}
+
+// Rows of q or dO whose tiles of 128 packed rows are addressed with 32-bit offsets.
+bool tile_rows(const upipe_heads& v, int G) {
+  const int64_t most = int64_t(1) << 30;
+  return v.row <= most / 256 && v.head <= most / (2 * G) &&
+         2 * (tile_tokens(G) * v.row + G * v.head) < most;
+}
 
 bool stage_rows(const upipe_heads& v) { return v.row <= kMaxRowStride; }
 
@@ -281,6 +453,10 @@ int upipe_varlen_plan(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int H
     memcpy(to, &p.h, sizeof(p.h));
     put(to, p.h.at_fwd, p.fwd);
     put(to, p.h.at_merge, p.merge);
+    put(to, p.h.at_term, p.terms);
+    put(to, p.h.at_key, p.keys);
+    put(to, p.h.at_fold, p.folds);
+    put(to, p.h.at_dq, p.dqs);
     return UPIPE_OK;
   } catch (...) {
     return UPIPE_ERR_HIP;
@@ -337,6 +513,81 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
       m.Hq = Hq;
       UPIPE_LAUNCH(kRowsMerge, stream, launch_rows_merge(m, h->n_merge, stream));
     }
+    return UPIPE_OK;
+  } catch (...) {
+    return UPIPE_ERR_HIP;
+  }
+}
+
+size_t upipe_attn_bwd_varlen_workspace_size(const void* plan) {
+  const PlanHeader* h = header_of(plan);
+  return h ? bwd_ws(*h) : 0;
+}
+
+int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_heads o,
+                          const float* lse, int64_t lse_head, upipe_heads dout, upipe_heads dq,
+                          upipe_heads dk, upipe_heads dv, const void* plan, const void* plan_dev,
+                          void* ws, size_t ws_bytes, hipStream_t stream) {
+  try {
+    const PlanHeader* h = header_of(plan);
+    if (!h || !aligned16(plan_dev)) return UPIPE_ERR_INVALID_ARG;
+    const int64_t Tq = h->total_q, Tk = h->total_k;
+    const int Hq = h->Hq, Hkv = h->Hkv, G = Hq / Hkv;
+    if (Tq == 0 && Tk == 0) return UPIPE_OK;
+    if (!aligned16(ws) || (Tq > 0 && (!aligned16(lse) || lse_head < Tq || lse_head > kMaxTokens)))
+      return UPIPE_ERR_INVALID_ARG;
+    const upipe_heads *rq[4] = {&q, &o, &dout, &dq}, *rk[4] = {&k, &v, &dk, &dv};
+    for (int i = 0; i < 4; ++i)
+      if ((Tq > 0 && !heads_ok(*rq[i], Tq, Hq)) || (Tk > 0 && !heads_ok(*rk[i], Tk, Hkv)))
+        return UPIPE_ERR_INVALID_ARG;
+    if ((Tq > 0 && !heads_distinct(dq, Tq, Hq)) ||
+        (Tk > 0 && (!heads_distinct(dk, Tk, Hkv) || !heads_distinct(dv, Tk, Hkv))))
+      return UPIPE_ERR_INVALID_ARG;
+    // dq may be q or dout: its kernel comes last, and reads a row before it writes it.
+    for (int i = 0; i < 3; ++i)
+      if ((!(i != 1 && heads_same(dq, *rq[i])) && !apart(dq, Tq, Hq, *rq[i], Tq, Hq)) ||
+          !apart(dk, Tk, Hkv, *rq[i], Tq, Hq) || !apart(dv, Tk, Hkv, *rq[i], Tq, Hq))
+        return UPIPE_ERR_INVALID_ARG;
+    for (int i = 0; i < 2; ++i)
+      if (!apart(dq, Tq, Hq, *rk[i], Tk, Hkv) || !apart(dk, Tk, Hkv, *rk[i], Tk, Hkv) ||
+          !apart(dv, Tk, Hkv, *rk[i], Tk, Hkv))
+        return UPIPE_ERR_INVALID_ARG;
+    if (!apart(dq, Tq, Hq, dk, Tk, Hkv) || !apart(dq, Tq, Hq, dv, Tk, Hkv) ||
+        !apart(dk, Tk, Hkv, dv, Tk, Hkv))
+      return UPIPE_ERR_INVALID_ARG;
+    if ((Tk > 0 && (!stage_rows(k) || !stage_rows(v))) ||
+        (Tq > 0 && (!tile_rows(q, G) || !tile_rows(dout, G))))
+      return UPIPE_ERR_UNSUPPORTED;
+    if (ws_bytes < bwd_ws(*h)) return UPIPE_ERR_WORKSPACE;
+    const char* dev = (const char*)plan_dev;
+    RowBwdArgs a{};
+    a.q = view_of(q);
+    a.k = view_of(k);
+    a.v = view_of(v);
+    a.o = view_of(o);
+    a.dO = view_of(dout);
+    a.dq = view_of(dq);
+    a.dk = view_of(dk);
+    a.dv = view_of(dv);
+    a.lse = lse;
+    a.lse_head = lse_head;
+    a.term_rows = h->term_rows;
+    a.D = (float*)ws;
+    a.lse_c = a.D + Hkv * h->term_rows;
+    a.sums = (float*)((char*)ws + sums_at(*h));
+    a.slots = h->slots;
+    a.terms = (const TermItem*)(dev + h->at_term);
+    a.keys = (const KeyItem*)(dev + h->at_key);
+    a.folds = (const FoldItem*)(dev + h->at_fold);
+    a.dqs = (const DqItem*)(dev + h->at_dq);
+    a.Hkv = Hkv;
+    a.G = G;
+    a.causal = h->causal;
+    if (h->n_term > 0) UPIPE_LAUNCH(kRowsTerms, stream, launch_rows_terms(a, h->n_term, stream));
+    if (h->n_key > 0) UPIPE_LAUNCH(kRowsDkdv, stream, launch_rows_dkdv(a, h->n_key, stream));
+    if (h->n_fold > 0)
+      UPIPE_LAUNCH(kRowsDkdvFold, stream, launch_rows_dkdv_fold(a, h->n_fold, stream));
+    if (h->n_dq > 0) UPIPE_LAUNCH(kRowsDq, stream, launch_rows_dq(h->dq_ks, a, h->n_dq, stream));
     return UPIPE_OK;
   } catch (...) {
     return UPIPE_ERR_HIP;

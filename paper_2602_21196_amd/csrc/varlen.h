@@ -93,4 +93,27 @@ struct RowMergeArgs {
 };
 hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t blocks, hipStream_t st);
 
+// ---- backward (varlen_bwd.hip) ---------------------------------------------
+struct RowBwdArgs {
+  HeadView q, k, v, o, dO, dq, dk, dv;
+  const float* lse;
+  int64_t lse_head;
+  // Row terms [Hkv][term_rows]: D = dO.o and -sqrt(d) lse of the packed rows, in tiles
+  // of 128 rows, tile_tokens(G) G of them used.
+  float *D, *lse_c;
+  int64_t term_rows;
+  float* sums;               // [Hkv][slots][2][128][128] sums of segments
+  int64_t slots;
+  const TermItem* terms;
+  const KeyItem* keys;
+  const FoldItem* folds;
+  const DqItem* dqs;
+  int Hkv, G, causal;
+};
+// n items of every key/value head.
+hipError_t launch_rows_terms(const RowBwdArgs& a, int64_t n, hipStream_t st);
+hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st);
+hipError_t launch_rows_dkdv_fold(const RowBwdArgs& a, int64_t n, hipStream_t st);
+hipError_t launch_rows_dq(int ks, const RowBwdArgs& a, int64_t n, hipStream_t st);
+
 }  // namespace upipe

@@ -87,6 +87,9 @@ _SIGNATURES = {
     "upipe_attn_fwd_varlen_workspace_size": (_size, [_c_void_p]),
     "upipe_attn_fwd_varlen": (_int, [upipe_heads] * 4 + [_fptr, _i64, _c_void_p, _c_void_p,
                                                          _c_void_p, _size, _c_void_p]),
+    "upipe_attn_bwd_varlen_workspace_size": (_size, [_c_void_p]),
+    "upipe_attn_bwd_varlen": (_int, [upipe_heads] * 4 + [_fptr, _i64] + [upipe_heads] * 4 +
+                              [_c_void_p, _c_void_p, _c_void_p, _size, _c_void_p]),
     "upipe_attn_decode_workspace_size": (_size, [_i64, _int, _i64, _i64, _int, _int, _int]),
     "upipe_attn_decode": (_int, [upipe_heads, upipe_heads, _i64, upipe_heads, _i64, _c_void_p,
                                  upipe_heads, upipe_heads, upipe_heads, _fptr, _i64, _int, _i64,
@@ -268,6 +271,16 @@ def upipe_attn_fwd_varlen_workspace_size(plan):
 def upipe_attn_fwd_varlen(q, k, v, o, lse, lse_head, plan, plan_dev, ws, ws_bytes, stream):
     return lib().upipe_attn_fwd_varlen(q, k, v, o, lse, lse_head, plan, plan_dev, ws, ws_bytes,
                                        stream)
+
+
+def upipe_attn_bwd_varlen_workspace_size(plan):
+    return lib().upipe_attn_bwd_varlen_workspace_size(plan)
+
+
+def upipe_attn_bwd_varlen(q, k, v, o, lse, lse_head, dout, dq, dk, dv, plan, plan_dev, ws, ws_bytes,
+                          stream):
+    return lib().upipe_attn_bwd_varlen(q, k, v, o, lse, lse_head, dout, dq, dk, dv, plan, plan_dev,
+                                       ws, ws_bytes, stream)
 
 
 def upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d):
@@ -754,6 +767,7 @@ class VarlenPlan:
         self.Hq, self.Hkv, self.causal = int(Hq), int(Hkv), bool(causal)
         self.total_q, self.total_k = cu_q[-1], cu_k[-1]
         self.fwd_workspace = upipe_attn_fwd_varlen_workspace_size(self.host)
+        self.bwd_workspace = upipe_attn_bwd_varlen_workspace_size(self.host)
         self.dev = torch.frombuffer(self._host, dtype=torch.uint8).to(device)
 
 
@@ -794,6 +808,31 @@ def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
                                    plan.host, plan.dev.data_ptr(), ws.data_ptr(), ws.numel(), stream)
     _check("upipe_attn_fwd_varlen", st)
     return o, lse
+
+
+def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
+    """(dq, dk, dv) of the packed q, k, v, with o and lse of attn_fwd_varlen and the
+    same plan.  Rows behind the last sequence are left as they are in out = (dq, dk, dv),
+    0 in new tensors; dq may be q or dout."""
+    torch = _torch()
+    Tq, Tk = plan.total_q, plan.total_k
+    views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
+             _packed(v, "v", Tk, plan.Hkv), _packed(o, "o", Tq, plan.Hq))
+    if out is None:
+        out = tuple(torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) for t in (q, k, v))
+        for t, n in zip(out, (Tq, Tk, Tk)):
+            if n < t.shape[0]:
+                t[n:] = 0
+    dq, dk, dv = out
+    grads = (_packed(dout, "dout", Tq, plan.Hq), _packed(dq, "dq", Tq, plan.Hq),
+             _packed(dk, "dk", Tk, plan.Hkv), _packed(dv, "dv", Tk, plan.Hkv))
+    ws = _workspace(ws, plan.bwd_workspace, q.device, "upipe_attn_bwd_varlen_workspace_size")
+    with _Call(q=q, k=k, v=v, o=o, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, plan=plan.dev,
+               ws=ws) as stream:
+        st = upipe_attn_bwd_varlen(*views, *_packed_lse(lse, q, plan), *grads, plan.host,
+                                   plan.dev.data_ptr(), ws.data_ptr(), ws.numel(), stream)
+    _check("upipe_attn_bwd_varlen", st)
+    return dq, dk, dv
 
 
 def _cache(t, name, B, Hkv):

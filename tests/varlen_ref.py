@@ -103,3 +103,19 @@ def check_forward(o, lse, ref, rows=slice(None)):
     check("o", o[rows], ref.o[rows], (BF16 * ref.o.abs() + (1 + BF16) * w * ref.a_o)[rows] + 1e-30)
     fin = torch.where(torch.isinf(ref.lse), 0.0, ref.lse)
     check("lse", lse[:, rows], ref.lse[:, rows], (es + 4 * FP32 * fin.abs() + 8 * FP32)[:, rows])
+
+
+def check_backward(dq, dk, dv, ref, rows_q=slice(None), rows_k=slice(None)):
+    """Half a step of each result, and: dv has half a step of every weight and the
+    weight's error (score, and lse, which has the score's error again); dS has that too, half
+    a step of its own, and D's error, which is o's: half a step of o and of the weights that
+    formed it.  All relative to the sums of absolute terms."""
+    es = float(score_error(ref.s_lse.max())) if ref.s_lse.numel() else 0.0
+    ep = 3 * es + 16 * FP32
+    cv = BF16 + (1 + BF16) * ep
+    cs = BF16 + ep + 2 * (BF16 + 2 * es + 8 * FP32) + 8 * BF16 * BF16 + (D + 8) * FP32
+    for name, got, want, size, c, rows in (("dq", dq, ref.dq, ref.a_dq, cs, rows_q),
+                                           ("dk", dk, ref.dk, ref.a_dk, cs, rows_k),
+                                           ("dv", dv, ref.dv, ref.a_dv, cv, rows_k)):
+        check(name, got[rows], want[rows],
+              (BF16 * want.abs() + (1 + BF16) * c * size)[rows] + 1e-30)
