@@ -274,15 +274,15 @@ __global__ __launch_bounds__(256, 1) void attn_bwd_dkdv_kernel(
     Frags fa;
     if (QS == 1) {
       read_sdp(buf, 96, r32, g, fa);
-      pair_step<CAUSAL, true, 1>(next, 0, buf, buf, 64, qb, kw, mykey, r32, g, lane, kf, vf, dva,
-                                 dka, fa);
-      pair_step<CAUSAL, false, 1>(next, 4, buf, lower, 0, qb, kw, mykey, r32, g, lane, kf,
-                                  vf, dva, dka, fa);
+      pair_step<CAUSAL, true, 1>(next, 0, TileRows{buf, buf, r32, g, lane}, 64, qb, kw, mykey, g, kf,
+                                 vf, dva, dka, fa);
+      pair_step<CAUSAL, false, 1>(next, 4, TileRows{buf, lower, r32, g, lane}, 0, qb, kw, mykey, g,
+                                  kf, vf, dva, dka, fa);
     } else {
       const int base = 64 * qs;
       read_sdp(buf, base + 32, r32, g, fa);
-      pair_step<CAUSAL, false, 2>(next, 0, buf, qs == 0 ? lower : buf, base, qb, kw, mykey, r32, g,
-                                  lane, kf, vf, dva, dka, fa);
+      pair_step<CAUSAL, false, 2>(next, 0, TileRows{buf, qs == 0 ? lower : buf, r32, g, lane}, base,
+                                  qb, kw, mykey, g, kf, vf, dva, dka, fa);
     }
     qt = nq;
     hh = nh;

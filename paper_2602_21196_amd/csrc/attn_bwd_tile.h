@@ -51,6 +51,15 @@ __device__ __forceinline__ void read_dvdk(const char* buf, int sub, int lane, Fr
     }
 }
 
+// A staged tile as pair_step reads it.
+struct TileRows {
+  const char* buf;
+  const char* dbuf;      // where the dV / dK products read their rows
+  int r32, g, lane;
+  __device__ __forceinline__ void sdp(int sub, Frags& fr) const { read_sdp(buf, sub, r32, g, fr); }
+  __device__ __forceinline__ void dvdk(int sub, Frags& fr) const { read_dvdk(dbuf, sub, lane, fr); }
+};
+
 // Accumulator seeds of the 32-row subtile at rows `sub`.. of the tile, in the
 // MFMA C layout (element 4a + b is row sub + 8a + 4g + b), loaded from the
 // staged rows straight into the accumulators: the score accumulator starts at
@@ -172,28 +181,26 @@ __device__ __forceinline__ void interleave_mfma_valu() {
 // tile's copies, from `blk` on.  The lower subtile is computed even where only
 // the upper one is needed: the diagonal mask then zeroes all of its P and dS.
 // So is a pair that this wave's keys do not see at all; its dV / dK products then
-// read the tile's upper pair (`dbuf` for `buf`), which the wave computes anyway:
+// read the tile's upper pair (Tile::dvdk), which the wave computes anyway:
 // what a zero P or dS does to those rows is done already, where a row of the
 // masked pair that holds an infinity or NaN would give 0 x NaN.
-template <bool CAUSAL, bool PF, int NB, class Copy>
-__device__ __forceinline__ void pair_step(const Copy& next, int blk, const char* buf,
-                                          const char* dbuf, int base, uint32_t qb, uint32_t kw,
-                                          uint32_t mykey,
-                                          int r32, int g, int lane, const bf16x8 (&kf)[8],
-                                          const bf16x8 (&vf)[8],
+template <bool CAUSAL, bool PF, int NB, class Copy, class Tile>
+__device__ __forceinline__ void pair_step(const Copy& next, int blk, const Tile& tile, int base,
+                                          uint32_t qb, uint32_t kw, uint32_t mykey, int g,
+                                          const bf16x8 (&kf)[8], const bf16x8 (&vf)[8],
                                           f32x16 (&dva)[4], f32x16 (&dka)[4], Frags& fa) {
   Frags fb;
   f32x16 s1, p1, s0, p0;
   bf16x8 pf1[2], sf1[2], pf0[2], sf0[2];
   const uint32_t q1 = qb + base + 32, q0 = qb + base;
-  subtile_seed(buf, base + 32, g, s1, p1);
-  subtile_seed(buf, base, g, s0, p0);
+  subtile_seed(tile.buf, base + 32, g, s1, p1);
+  subtile_seed(tile.buf, base, g, s0, p0);
   __builtin_amdgcn_sched_barrier(0);
-  read_sdp(buf, base, r32, g, fb);
+  tile.sdp(base, fb);
   __builtin_amdgcn_sched_barrier(0);
   next.blocks(blk, 2 * NB);
   subtile_sdp(fa, kf, vf, s1, p1);                                            // A
-  read_dvdk(dbuf, base + 32, lane, fa);
+  tile.dvdk(base + 32, fa);
   interleave_mfma_lds<2>();
   __builtin_amdgcn_sched_barrier(0);
   subtile_sdp(fb, kf, vf, s0, p0);                                            // B
@@ -202,7 +209,7 @@ __device__ __forceinline__ void pair_step(const Copy& next, int blk, const char*
   __builtin_amdgcn_sched_barrier(0);
   subtile_mask<CAUSAL>(q1, mykey, q1 < kw + 31, g, pf1, sf1);
   dvdk_products(fa, pf1, sf1, dva, dka);                                      // C
-  read_dvdk(dbuf, base, lane, fb);
+  tile.dvdk(base, fb);
   subtile_pds(s0, p0, pf0, sf0);
   interleave_mfma_valu();
   __builtin_amdgcn_sched_barrier(0);
@@ -210,7 +217,7 @@ __device__ __forceinline__ void pair_step(const Copy& next, int blk, const char*
   next.blocks(blk + 2 * NB, 2 * NB);
   dvdk_products(fb, pf0, sf0, dva, dka);                                      // D
   if (PF) {   // the next pair's upper subtile
-    read_sdp(buf, base - 32, r32, g, fa);
+    tile.sdp(base - 32, fa);
     interleave_mfma_lds<1>();
   }
 }

@@ -21,16 +21,16 @@ namespace upipe {
 
 namespace {
 
-// 128 rows of one tile; sixteen lanes a row.  Rows that see no key get zeros: every
-// pair of theirs is masked, and zeros keep what is masked finite.
+// 32 rows of one tile of 128; sixteen lanes a row.  Rows that see no key get zeros:
+// every pair of theirs is masked, and zeros keep what is masked finite.
 __global__ __launch_bounds__(256) void rows_terms_kernel(RowBwdArgs a) {
-  const int kvh = blockIdx.x % a.Hkv;
-  const TermItem it = a.terms[blockIdx.x / a.Hkv];
+  const int kvh = blockIdx.x / 4 % a.Hkv;
+  const TermItem it = a.terms[blockIdx.x / 4 / a.Hkv];
   const int c = threadIdx.x & 15, G = a.G, tpt = tile_tokens(G);
   const int64_t out = kvh * a.term_rows + it.r0 + it.tile * 128;
-#pragma unroll 2
-  for (int i = 0; i < 8; ++i) {
-    const int r = 16 * i + (threadIdx.x >> 4);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int r = 32 * (blockIdx.x % 4) + 16 * i + (threadIdx.x >> 4);
     const int t = r / G, tok = it.tile * tpt + t, h = kvh * G + r - t * G;
     float acc = 0.f, l = -INFINITY;
     if (t < tpt && tok < it.Lq) {
@@ -54,33 +54,45 @@ __global__ __launch_bounds__(256) void rows_terms_kernel(RowBwdArgs a) {
 
 // ------------------------------------------------------------------ dK / dV
 // The copies of one tile by one wave, as the products' kernel wants them
-// (attn_bwd_tile.h): KV_BLK blocks of four rows of Q and of dO, and the row terms.
+// (attn_bwd_tile.h): KV_BLK blocks of four rows of Q and of dO, and the row terms.  A
+// lane's places in a tile are the same for all tiles and kept.  INSIDE: the rows of a
+// token do not reach into the next token's, so what lies behind the last token is cut off
+// by the sources' sizes; else (head-major rows) every lane asks.
+template <bool INSIDE>
 struct RowCopy {
   i32x4 q, dO, lse, D;       // of the tile
-  uint32_t q_row, q_head, d_row, d_head;     // bytes
+  uint32_t at_q[KV_BLK], at_d[KV_BLK];     // this lane's 16 bytes of every block
   uint32_t per_g;            // ceil(2^16 / G)
-  int G, tokens;             // heads of the group, valid tokens of the tile
+  int tokens;                // valid tokens of the tile
   uint32_t lds;
-  int w, sub, chunk;         // this lane's row of a block, and its 16 bytes of the row
+  int w;
 
-  __device__ __forceinline__ void offsets(int i, int s, uint32_t& oq, uint32_t& od) const {
-    const uint32_t r = 4 * (KV_BLK * w + i) + s;
-    const uint32_t t = (r * per_g) >> 16, h = r - t * G;      // r / G for r < 128
-    const uint32_t c = (uint32_t)(chunk ^ (s << 2) ^ (i & 3)) << 4;    // tsw(r)
-    const bool ok = (int)t < tokens;       // else no row: zeros
-    oq = ok ? t * q_row + h * q_head + c : 0x80000000u;
-    od = ok ? t * d_row + h * d_head + c : 0x80000000u;
+  __device__ __forceinline__ void init(int wave, int lane, int G, const HeadView& Q,
+                                       const HeadView& dOv) {
+    w = wave;
+    per_g = (65536 + G - 1) / G;
+#pragma unroll
+    for (int i = 0; i < KV_BLK; ++i) {
+      const uint32_t r = 4 * (KV_BLK * w + i) + (lane >> 4);
+      const uint32_t t = (r * per_g) >> 16, h = r - t * G;      // r / G for r < 128
+      const uint32_t c = ((lane & 15) ^ tsw(r)) << 4;
+      at_q[i] = (t * (uint32_t)Q.row + h * (uint32_t)Q.head) * 2 + c;
+      at_d[i] = (t * (uint32_t)dOv.row + h * (uint32_t)dOv.head) * 2 + c;
+    }
   }
   // Blocks i0 .. i0 + n - 1 of this wave's (both even).
   __device__ __forceinline__ void blocks(int i0, int n) const {
-    int s = sub;
-    asm volatile("" : "+v"(s));      // formed anew for every tile: kept, they would spill
+    auto ok = [&](int i) {
+      const uint32_t r = 4 * (KV_BLK * w + i) + ((threadIdx.x & 63) >> 4);
+      return INSIDE || (int)((r * per_g) >> 16) < tokens;      // else no row: zeros
+    };
 #pragma unroll
     for (int i = i0; i < i0 + n; i += 2) {
-      uint32_t q0, q1, d0, d1;
-      offsets(i, s, q0, d0);
-      offsets(i + 1, s, q1, d1);
-      copy2x2_b128<OFF_DO - OFF_Q>(q, dO, q0, q1, d0, d1, lds + OFF_Q + (KV_BLK * w + i) * 1024);
+      const bool ok0 = ok(i), ok1 = ok(i + 1);
+      copy2x2_b128<OFF_DO - OFF_Q>(q, dO, ok0 ? at_q[i] : 0x80000000u,
+                                   ok1 ? at_q[i + 1] : 0x80000000u, ok0 ? at_d[i] : 0x80000000u,
+                                   ok1 ? at_d[i + 1] : 0x80000000u,
+                                   lds + OFF_Q + (KV_BLK * w + i) * 1024);
     }
   }
   __device__ __forceinline__ void rows(int lane) const {
@@ -91,6 +103,30 @@ struct RowCopy {
   }
 };
 
+// A staged tile by two per-lane places and exclusive-ors (common.h): a register for
+// every address would spill.
+struct PlacedTile {
+  const char *buf, *smem;
+  uint32_t sdp_at, tr;       // of this lane's chunk of row r32, of its transposing reads
+  __device__ __forceinline__ void sdp(int sub, Frags& fr) const {
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      fr.f[2 * s] = lds_read_b128(smem, (sdp_at ^ (32 * s)) + OFF_Q + sub * 256);
+      fr.f[2 * s + 1] = lds_read_b128(smem, (sdp_at ^ (32 * s)) + OFF_DO + sub * 256);
+    }
+  }
+  __device__ __forceinline__ void dvdk(int sub, Frags& fr) const {
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) {
+        fr.f[4 * dt + 2 * kt] = tr_operand_at(smem, tr, sub + 16 * kt + OFF_DO / 256, dt);
+        fr.f[4 * dt + 2 * kt + 1] = tr_operand_at(smem, tr, sub + 16 * kt + OFF_Q / 256, dt);
+      }
+  }
+};
+
+template <bool INSIDE>
 __global__ __launch_bounds__(256, 1) void rows_dkdv_kernel(RowBwdArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[2 * KV_STAGE];
   const int t = threadIdx.x;
@@ -107,30 +143,27 @@ __global__ __launch_bounds__(256, 1) void rows_dkdv_kernel(RowBwdArgs a) {
   const uint32_t sees_w0 = first_row(kw), sees_w31 = first_row(kw + 31), sees = first_row(mykey);
 
   const uint32_t lds0 = lds_address(smem);
-  RowCopy next;
-  next.q_row = (uint32_t)(a.q.row * 2);
-  next.q_head = (uint32_t)(a.q.head * 2);
-  next.d_row = (uint32_t)(a.dO.row * 2);
-  next.d_head = (uint32_t)(a.dO.head * 2);
-  next.per_g = (65536 + G - 1) / G;
-  next.G = G;
-  next.w = w;
-  next.sub = lane >> 4;
-  next.chunk = lane & 15;
+  RowCopy<INSIDE> next;
+  next.init(w, lane, G, a.q, a.dO);
   const bf16* qh = a.q.p + it.q0 * a.q.row + kvh * G * a.q.head;
   const bf16* dh = a.dO.p + it.q0 * a.dO.row + kvh * G * a.dO.head;
   const float* lh = a.lse_c + kvh * a.term_rows + it.r0;
   const float* Dh = a.D + kvh * a.term_rows + it.r0;
-  // Tile qt to the stage at `lds`; past the walk's end nothing (zeros).
+  // Tile qt to the stage at `lds`; past the walk's end tile 0 with sizes of none (zeros).
+  // INSIDE: sizes up to the end of the last token's rows.
+  const uint32_t q_row = (uint32_t)a.q.row * 2, q_in = (uint32_t)((G - 1) * a.q.head + HEAD_DIM) * 2;
+  const uint32_t d_row = (uint32_t)a.dO.row * 2, d_in = (uint32_t)((G - 1) * a.dO.head + HEAD_DIM) * 2;
   auto aim = [&](int qt, bool some, uint32_t lds) {
-    const int64_t tok = some ? (int64_t)qt * tpt : 0;
+    const uint32_t on = some ? 0xffffffffu : 0u;
+    const int tile = qt & (int)on;
+    const int64_t tok = (int64_t)tile * tpt;
     next.tokens = min(tpt, it.Lq - (int)tok);
-    // the offsets keep to the sequence's rows; the sizes only turn the copies off
-    const uint32_t most = some ? 0x7fffffffu : 0;
-    next.q = rsrc_words(qh + tok * a.q.row, most);
-    next.dO = rsrc_words(dh + tok * a.dO.row, most);
-    next.lse = rsrc_words(lh + (some ? qt * QT : 0), some ? QT * 4 : 0);
-    next.D = rsrc_words(Dh + (some ? qt * QT : 0), some ? QT * 4 : 0);
+    next.q = rsrc_words(qh + tok * a.q.row,
+                        (INSIDE ? (next.tokens - 1) * q_row + q_in : 0x7fffffffu) & on);
+    next.dO = rsrc_words(dh + tok * a.dO.row,
+                         (INSIDE ? (next.tokens - 1) * d_row + d_in : 0x7fffffffu) & on);
+    next.lse = rsrc_words(lh + (int64_t)tile * QT, (QT * 4) & on);
+    next.D = rsrc_words(Dh + (int64_t)tile * QT, (QT * 4) & on);
     next.lds = lds;
   };
   aim(it.first, it.count > 0, lds0);
@@ -168,7 +201,13 @@ __global__ __launch_bounds__(256, 1) void rows_dkdv_kernel(RowBwdArgs a) {
       dka[dt][i] = 0.f;
       dva[dt][i] = 0.f;
     }
+  // Zeros that the compiler does not know for zeros: knowing them it keeps half of the
+  // sums in VGPRs, swaps them with AGPRs in every tile and spills addresses (dK/dV of
+  // 131072 rows of 4 heads 37.8 ms).
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt) asm volatile("" : "+a"(dka[dt]), "+a"(dva[dt]));
 
+  const uint32_t sdp_lane = swzt(r32, g), tr_lane = tr_base(lane);
   for (int n = 0; n < it.count; ++n) {
     const char* buf = smem + (n & 1) * KV_STAGE;
     const uint32_t qb = (uint32_t)(it.first - n) * (tpt * G);    // first row of the tile
@@ -178,13 +217,13 @@ __global__ __launch_bounds__(256, 1) void rows_dkdv_kernel(RowBwdArgs a) {
     next.rows(lane);
     // Pairs of 32-row subtiles, upper rows first.  A pair that this wave's keys do not
     // see is computed too, masked whole, on the rows of the other pair.
-    const char* lower = buf + (qb + 63 < sees_w0 ? 64 * HEAD_DIM * 2 : 0);
+    const uint32_t boff = (n & 1) * KV_STAGE;
+    PlacedTile upper{buf, smem, sdp_lane + boff, tr_lane + boff}, lower = upper;
+    if (qb + 63 < sees_w0) lower.tr += 64 * HEAD_DIM * 2;
     Frags fa;
-    read_sdp(buf, 96, r32, g, fa);
-    pair_step<true, true, 1>(next, 0, buf, buf, 64, qb, sees_w31 - 31, sees, r32, g, lane, kf, vf,
-                             dva, dka, fa);
-    pair_step<true, false, 1>(next, 4, buf, lower, 0, qb, sees_w31 - 31, sees, r32, g, lane, kf, vf,
-                              dva, dka, fa);
+    upper.sdp(96, fa);
+    pair_step<true, true, 1>(next, 0, upper, 64, qb, sees_w31 - 31, sees, g, kf, vf, dva, dka, fa);
+    pair_step<true, false, 1>(next, 4, lower, 0, qb, sees_w31 - 31, sees, g, kf, vf, dva, dka, fa);
   }
 
   wait_vmem();      // the last tile's empty copies (to LDS) have ended
@@ -444,12 +483,17 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
 }  // namespace
 
 hipError_t launch_rows_terms(const RowBwdArgs& a, int64_t n, hipStream_t st) {
-  hipLaunchKernelGGL(rows_terms_kernel, dim3((unsigned)(n * a.Hkv)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(rows_terms_kernel, dim3((unsigned)(n * a.Hkv * 4)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st) {
-  hipLaunchKernelGGL(rows_dkdv_kernel, dim3((unsigned)(n * a.Hkv)), dim3(256), 0, st, a);
+  auto inside = [&](const HeadView& v) { return v.row >= (a.G - 1) * v.head + HEAD_DIM; };
+  const dim3 grid((unsigned)(n * a.Hkv));
+  if (inside(a.q) && inside(a.dO))
+    hipLaunchKernelGGL(rows_dkdv_kernel<true>, grid, dim3(256), 0, st, a);
+  else
+    hipLaunchKernelGGL(rows_dkdv_kernel<false>, grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -1,0 +1,470 @@
+// Attention backward over packed sequences of different lengths, for gfx950.
+//
+//   P_ij  = exp(q_i.k_j / sqrt d - lse_i),   D_i = dO_i . o_i,
+//   dS_ij = P_ij (dO_i . v_j - D_i),         dV_j = sum_i P_ij dO_i,
+//   dK_j  = sum_i dS_ij q_i / sqrt d,        dQ_i = sum_j dS_ij k_j / sqrt d
+// over the visible pairs of each sequence; P and dS are rounded to bf16 for their
+// products (as the matrix instructions take them), all sums are fp32.  The rows of
+// a key/value group are packed (varlen.h), so dK and dV sum over the group's heads by
+// walking its rows.  No atomics: every sum has a fixed order.
+//   terms: D and -sqrt(d) lse of the packed rows, in tiles of 128
+//   dkdv:  a workgroup owns 128 keys of one key/value head and walks the tiles of
+//          rows that see them, from the last one down; long walks are cut into
+//          segments side by side, whose sums are added in their order
+//   dq:    a workgroup owns 256, 128 or 64 packed rows and walks stages of keys
+// The products of a tile are those of the backward over equal lengths
+// (attn_bwd_tile.h).
+#include "attn_bwd_tile.h"
+#include "varlen.h"
+
+namespace upipe {
+
+namespace {
+
+// 128 rows of one tile; sixteen lanes a row.  Rows that see no key get zeros: every
+// pair of theirs is masked, and zeros keep what is masked finite.
+__global__ __launch_bounds__(256) void rows_terms_kernel(RowBwdArgs a) {
+  const int kvh = blockIdx.x % a.Hkv;
+  const TermItem it = a.terms[blockIdx.x / a.Hkv];
+  const int c = threadIdx.x & 15, G = a.G, tpt = tile_tokens(G);
+  const int64_t out = kvh * a.term_rows + it.r0 + it.tile * 128;
+#pragma unroll 2
+  for (int i = 0; i < 8; ++i) {
+    const int r = 16 * i + (threadIdx.x >> 4);
+    const int t = r / G, tok = it.tile * tpt + t, h = kvh * G + r - t * G;
+    float acc = 0.f, l = -INFINITY;
+    if (t < tpt && tok < it.Lq) {
+      l = a.lse[h * a.lse_head + it.q0 + tok];
+      const bf16x8 x = *reinterpret_cast<const bf16x8*>(
+          a.dO.p + (it.q0 + tok) * a.dO.row + h * a.dO.head + 8 * c);
+      const bf16x8 y = *reinterpret_cast<const bf16x8*>(
+          a.o.p + (it.q0 + tok) * a.o.row + h * a.o.head + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc = fmaf((float)x[e], (float)y[e], acc);
+    }
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) acc += __shfl_xor(acc, off);
+    if (c == 0) {
+      const bool none = l == -INFINITY;
+      a.D[out + r] = none ? 0.f : acc;
+      a.lse_c[out + r] = none ? 0.f : l * -11.313708498984761f;     // -sqrt(128) lse
+    }
+  }
+}
+
+// ------------------------------------------------------------------ dK / dV
+// The copies of one tile by one wave, as the products' kernel wants them
+// (attn_bwd_tile.h): KV_BLK blocks of four rows of Q and of dO, and the row terms.
+struct RowCopy {
+  i32x4 q, dO, lse, D;       // of the tile
+  uint32_t q_row, q_head, d_row, d_head;     // bytes
+  uint32_t per_g;            // ceil(2^16 / G)
+  int G, tokens;             // heads of the group, valid tokens of the tile
+  uint32_t lds;
+  int w, sub, chunk;         // this lane's row of a block, and its 16 bytes of the row
+
+  __device__ __forceinline__ void offsets(int i, int s, uint32_t& oq, uint32_t& od) const {
+    const uint32_t r = 4 * (KV_BLK * w + i) + s;
+    const uint32_t t = (r * per_g) >> 16, h = r - t * G;      // r / G for r < 128
+    const uint32_t c = (uint32_t)(chunk ^ (s << 2) ^ (i & 3)) << 4;    // tsw(r)
+    const bool ok = (int)t < tokens;       // else no row: zeros
+    oq = ok ? t * q_row + h * q_head + c : 0x80000000u;
+    od = ok ? t * d_row + h * d_head + c : 0x80000000u;
+  }
+  // Blocks i0 .. i0 + n - 1 of this wave's (both even).
+  __device__ __forceinline__ void blocks(int i0, int n) const {
+    int s = sub;
+    asm volatile("" : "+v"(s));      // formed anew for every tile: kept, they would spill
+#pragma unroll
+    for (int i = i0; i < i0 + n; i += 2) {
+      uint32_t q0, q1, d0, d1;
+      offsets(i, s, q0, d0);
+      offsets(i + 1, s, q1, d1);
+      copy2x2_b128<OFF_DO - OFF_Q>(q, dO, q0, q1, d0, d1, lds + OFF_Q + (KV_BLK * w + i) * 1024);
+    }
+  }
+  __device__ __forceinline__ void rows(int lane) const {
+    if (lane < QT / 4) {
+      if (w == 0) copy_b128(lse, lane * 16u, 0, lds + OFF_LSE);
+      else if (w == 1) copy_b128(D, lane * 16u, 0, lds + OFF_D);
+    }
+  }
+};
+
+__global__ __launch_bounds__(256, 1) void rows_dkdv_kernel(RowBwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * KV_STAGE];
+  const int t = threadIdx.x;
+  const int lane = t & 63;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int r32 = lane & 31, g = lane >> 5;
+  const int kvh = blockIdx.x % a.Hkv, G = a.G, tpt = tile_tokens(G);
+  const KeyItem it = a.keys[blockIdx.x / a.Hkv];
+  const int kw = 128 * it.kb + 32 * w, mykey = kw + r32;
+  // First packed row that sees a key: the diagonal, within the sequence's rows.
+  auto first_row = [&](int key) {
+    return (uint32_t)(a.causal ? min(max(key - (it.Lk - it.Lq), 0), it.Lq) * G : 0);
+  };
+  const uint32_t sees_w0 = first_row(kw), sees_w31 = first_row(kw + 31), sees = first_row(mykey);
+
+  const uint32_t lds0 = lds_address(smem);
+  RowCopy next;
+  next.q_row = (uint32_t)(a.q.row * 2);
+  next.q_head = (uint32_t)(a.q.head * 2);
+  next.d_row = (uint32_t)(a.dO.row * 2);
+  next.d_head = (uint32_t)(a.dO.head * 2);
+  next.per_g = (65536 + G - 1) / G;
+  next.G = G;
+  next.w = w;
+  next.sub = lane >> 4;
+  next.chunk = lane & 15;
+  const bf16* qh = a.q.p + it.q0 * a.q.row + kvh * G * a.q.head;
+  const bf16* dh = a.dO.p + it.q0 * a.dO.row + kvh * G * a.dO.head;
+  const float* lh = a.lse_c + kvh * a.term_rows + it.r0;
+  const float* Dh = a.D + kvh * a.term_rows + it.r0;
+  // Tile qt to the stage at `lds`; past the walk's end nothing (zeros).
+  auto aim = [&](int qt, bool some, uint32_t lds) {
+    const int64_t tok = some ? (int64_t)qt * tpt : 0;
+    next.tokens = min(tpt, it.Lq - (int)tok);
+    // the offsets keep to the sequence's rows; the sizes only turn the copies off
+    const uint32_t most = some ? 0x7fffffffu : 0;
+    next.q = rsrc_words(qh + tok * a.q.row, most);
+    next.dO = rsrc_words(dh + tok * a.dO.row, most);
+    next.lse = rsrc_words(lh + (some ? qt * QT : 0), some ? QT * 4 : 0);
+    next.D = rsrc_words(Dh + (some ? qt * QT : 0), some ? QT * 4 : 0);
+    next.lds = lds;
+  };
+  aim(it.first, it.count > 0, lds0);
+  next.rows(lane);
+  next.blocks(0, KV_BLK);
+
+  // K and -V B-operand fragments (lane = key column, k = head dim); -V makes
+  // the dP products count down from D.  Keys past the last repeat it; their sums
+  // are not used.
+  bf16x8 kf[8], vf[8];
+  {
+    const int64_t key = it.k0 + min(mykey, it.Lk - 1);
+    const bf16* kp = a.k.p + key * a.k.row + kvh * a.k.head + 8 * g;
+    const bf16* vp = a.v.p + key * a.v.row + kvh * a.v.head + 8 * g;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      kf[s] = *reinterpret_cast<const bf16x8*>(kp + 16 * s);
+      vf[s] = -*reinterpret_cast<const bf16x8*>(vp + 16 * s);
+    }
+    // Only ever MFMA operands, which may come from AGPRs: the VGPRs are left to
+    // the score accumulators and the P / dS arithmetic.
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      asm volatile("" : "+a"(kf[s]));
+      asm volatile("" : "+a"(vf[s]));
+    }
+  }
+  // C layout: lane = head-dim column 32*dt + r32, element i = key row
+  // kw + 8*(i/4) + 4*g + (i%4).
+  f32x16 dka[4], dva[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      dka[dt][i] = 0.f;
+      dva[dt][i] = 0.f;
+    }
+
+  for (int n = 0; n < it.count; ++n) {
+    const char* buf = smem + (n & 1) * KV_STAGE;
+    const uint32_t qb = (uint32_t)(it.first - n) * (tpt * G);    // first row of the tile
+    wait_vmem();
+    __syncthreads();   // this tile landed for all waves; the other buffer is free
+    aim(it.first - n - 1, n + 1 < it.count, lds0 + ((n + 1) & 1) * KV_STAGE);
+    next.rows(lane);
+    // Pairs of 32-row subtiles, upper rows first.  A pair that this wave's keys do not
+    // see is computed too, masked whole, on the rows of the other pair.
+    const char* lower = buf + (qb + 63 < sees_w0 ? 64 * HEAD_DIM * 2 : 0);
+    Frags fa;
+    read_sdp(buf, 96, r32, g, fa);
+    pair_step<true, true, 1>(next, 0, buf, buf, 64, qb, sees_w31 - 31, sees, r32, g, lane, kf, vf,
+                             dva, dka, fa);
+    pair_step<true, false, 1>(next, 4, buf, lower, 0, qb, sees_w31 - 31, sees, r32, g, lane, kf, vf,
+                              dva, dka, fa);
+  }
+
+  wait_vmem();      // the last tile's empty copies (to LDS) have ended
+  if (it.slot >= 0) {
+    float* pk = a.sums + (kvh * a.slots + it.slot) * (2 * 128 * HEAD_DIM) + 32 * w * HEAD_DIM;
+    float* pv = pk + 128 * HEAD_DIM;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t off = (8 * (i >> 2) + 4 * g + (i & 3)) * HEAD_DIM + 32 * dt + r32;
+        pk[off] = dka[dt][i];
+        pv[off] = dva[dt][i];
+      }
+    return;
+  }
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int key = kw + 8 * (i >> 2) + 4 * g + (i & 3);
+      if (key < it.Lk) {
+        const int64_t at = it.k0 + key;
+        a.dk.p[at * a.dk.row + kvh * a.dk.head + 32 * dt + r32] = (bf16)(dka[dt][i] * -kScale);
+        a.dv.p[at * a.dv.row + kvh * a.dv.head + 32 * dt + r32] = (bf16)dva[dt][i];
+      }
+    }
+}
+
+// The segments' sums of a key block, added in the order of its walk: 16 workgroups a
+// block, a thread has eight consecutive elements of one key's dK or dV.
+__global__ __launch_bounds__(256) void rows_dkdv_fold_kernel(RowBwdArgs a) {
+  const int kvh = blockIdx.y;
+  const FoldItem it = a.folds[blockIdx.x / 16];
+  const int e8 = ((blockIdx.x % 16) * 256 + threadIdx.x) * 8;      // in [2][128][128]
+  const float* p = a.sums + (kvh * a.slots + it.slot) * (2 * 128 * HEAD_DIM) + e8;
+  f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll 4
+  for (int i = 0; i < it.n; ++i, p += 2 * 128 * HEAD_DIM) {
+    lo += *reinterpret_cast<const f32x4*>(p);
+    hi += *reinterpret_cast<const f32x4*>(p + 4);
+  }
+  const bool is_v = e8 >= 128 * HEAD_DIM;
+  const int key = 128 * it.kb + (e8 / HEAD_DIM) % 128, e = e8 % HEAD_DIM;
+  if (key >= it.Lk) return;
+  const float f = is_v ? 1.f : -kScale;
+  bf16x8 out;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    out[i] = (bf16)(lo[i] * f);
+    out[4 + i] = (bf16)(hi[i] * f);
+  }
+  const HeadView& d = is_v ? a.dv : a.dk;
+  *reinterpret_cast<bf16x8*>(d.p + (it.k0 + key) * d.row + kvh * d.head + e) = out;
+}
+
+// ---------------------------------------------------------------------- dQ
+// Eight waves of 32 packed rows x a part of every stage's keys: 256 rows x 64-key
+// stages, or, with the keys of 128-key stages in 2 or 4 parts, 128 or 64 rows, whose
+// sums are added in fp32 through LDS.
+template <int KS>
+struct DqTile {
+  static constexpr int NQW = 8 / KS;                // waves along the rows
+  static constexpr int BQ = 32 * NQW;               // rows per workgroup
+  static constexpr int BK = KS == 1 ? 64 : 128;     // keys per stage
+  static constexpr int NH = BK / 32 / KS;           // 32-key blocks of a stage per wave
+  static constexpr int T = BK * HEAD_DIM * 2;
+  static constexpr int OFF_K = 0, OFF_V = T;
+  static constexpr int STAGE = 2 * T;
+  static constexpr int BLK = T / 1024 / 8;          // 1 KB blocks per wave per tensor
+};
+constexpr int DQ_LA = 4;     // K/V fragment reads kept in flight
+
+template <int KS>
+__global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
+  using T = DqTile<KS>;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * T::STAGE];
+  const int t = threadIdx.x;
+  const int lane = t & 63;
+  const int w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wq = KS == 1 ? w : w % T::NQW, ks = KS == 1 ? 0 : w / T::NQW;
+  const int r32 = lane & 31, g = lane >> 5;
+  const int kvh = blockIdx.x % a.Hkv, G = a.G;
+  const DqItem it = a.dqs[blockIdx.x / a.Hkv];
+  const int n_rows = it.Lq * G, delta = it.Lk - it.Lq;
+  const int r0 = it.tile * T::BQ, rw = r0 + 32 * wq;
+  const int row = min(rw + r32, n_rows - 1);     // rows past the last compute on it
+  const int tok = row / G, hg = row - tok * G;
+
+  const uint32_t kb_row = (uint32_t)(a.k.row * 2), vb_row = (uint32_t)(a.v.row * 2);
+  const bf16* kp = a.k.p + it.k0 * a.k.row + kvh * a.k.head;
+  const bf16* vp = a.v.p + it.k0 * a.v.row + kvh * a.v.head;
+  const uint32_t lds0 = lds_address(smem);
+  uint32_t offk[T::BLK], offv[T::BLK];
+#pragma unroll
+  for (int i = 0; i < T::BLK; ++i) {
+    const int r = 4 * (T::BLK * w + i) + (lane >> 4);      // row of the tile, 16 lanes per row
+    const uint32_t c = ((lane & 15) ^ tsw(r)) << 4;
+    offk[i] = r * kb_row + c;
+    offv[i] = r * vb_row + c;
+  }
+  auto last_key = [&](int tk) { return a.causal ? min(tk + delta, it.Lk - 1) : it.Lk - 1; };
+  const int seen = last_key((min(r0 + T::BQ, n_rows) - 1) / G) + 1;
+  const int nst = max(0, (seen + T::BK - 1) / T::BK);
+  auto source = [&](const bf16* p, int64_t row_elems, int j) {
+    const int n = j < nst ? min(T::BK, it.Lk - j * T::BK) : 0;
+    return rsrc_words(p + (int64_t)j * T::BK * row_elems,
+                      n > 0 ? (uint32_t)((n - 1) * (int)row_elems + HEAD_DIM) * 2 : 0);
+  };
+  auto issue = [&](i32x4 rk, i32x4 rv, int i, uint32_t lds) {
+    copy2x2_b128<T::OFF_V - T::OFF_K>(rk, rv, offk[i], offk[i + 1], offv[i], offv[i + 1],
+                                      lds + T::OFF_K + (T::BLK * w + i) * 1024);
+  };
+  {
+    const i32x4 rk = source(kp, a.k.row, 0), rv = source(vp, a.v.row, 0);
+#pragma unroll
+    for (int i = 0; i < T::BLK; i += 2) issue(rk, rv, i, lds0);
+  }
+
+  bf16x8 qf[8], df[8];
+  float nlse, Dq;   // nlse = -sqrt(d) lse: the score accumulator's seed
+  {
+    const int h = kvh * G + hg, tpt = tile_tokens(G);
+    const bf16* qp = a.q.p + (it.q0 + tok) * a.q.row + h * a.q.head + 8 * g;
+    const bf16* dp = a.dO.p + (it.q0 + tok) * a.dO.row + h * a.dO.head + 8 * g;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s);
+      df[s] = *reinterpret_cast<const bf16x8*>(dp + 16 * s);
+    }
+    const int64_t term =
+        kvh * a.term_rows + it.r0 + (int64_t)(tok / tpt) * 128 + (tok % tpt) * G + hg;
+    nlse = a.lse_c[term];
+    Dq = a.D[term];
+  }
+
+  f32x16 qacc[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) qacc[dt][i] = 0.f;
+
+  const int k_part = 32 * T::NH * ks;        // first key of this wave's part of a stage
+  const uint32_t k_lane = T::OFF_K + k_part * 256 + swzt(r32, g);
+  const uint32_t v_lane = T::OFF_V + k_part * 256 + swzt(r32, g);
+  const uint32_t t_lane = T::OFF_K + k_part * 256 + tr_base(lane);
+  const int lim = last_key(tok), lim_w = last_key(rw / G);
+  // Stages with a key of this wave's part that a row of it may see come first.
+  const int seen_w = last_key((min(rw + 32, n_rows) - 1) / G) + 1;
+  const int nw = rw >= n_rows ? 0 : max(0, min(nst, (seen_w - k_part + T::BK - 1) / T::BK));
+  int j = 0;
+  for (; j < nw; ++j) {
+    const uint32_t boff = (j & 1) * T::STAGE;
+    wait_vmem();
+    __syncthreads();   // tile j landed for all waves; tile j-1's buffer is free
+    const uint32_t nlds = lds0 + ((j + 1) & 1) * T::STAGE;
+    const i32x4 nk = source(kp, a.k.row, j + 1), nv = source(vp, a.v.row, j + 1);
+    const int kb = j * T::BK + k_part;
+    const bool diag = kb + 32 * T::NH - 1 > lim_w;
+    // 32 keys at a time: one score and one dP accumulator live at a time, which leaves
+    // registers for DQ_LA fragment reads in flight ahead of the S / dP MFMAs.  The
+    // fragment addresses are exclusive-ors of three bases.
+    const uint32_t ka = k_lane + boff, va = v_lane + boff, ta = t_lane + boff;
+#pragma unroll
+    for (int hh = 0; hh < T::NH; ++hh) {
+      f32x16 sacc, pacc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) { sacc[i] = nlse; pacc[i] = 0.f; }
+#pragma unroll
+      for (int s = 0; s < 8; ++s) {
+        sacc = mfma32x32x16(lds_read_b128(smem, (ka ^ (32 * s)) + 8192 * hh), qf[s], sacc);
+        pacc = mfma32x32x16(lds_read_b128(smem, (va ^ (32 * s)) + 8192 * hh), df[s], pacc);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, DQ_LA, 0);
+#pragma unroll
+      for (int i = 0; i < 16 - DQ_LA; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, DQ_LA, 0);
+      // The next tile's copies go out behind the products they can hide behind.
+      if (hh == 0) issue(nk, nv, 0, nlds);
+      if (T::BLK > 2 && hh == T::NH - 1) issue(nk, nv, 2, nlds);
+      float ds[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(sacc[i] * kSl2) * (pacc[i] - Dq);
+      if (diag) {   // wave-uniform; by selection: masked, they may be inf or NaN
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (kb + 32 * hh + 8 * (i >> 2) + 4 * g + (i & 3) > lim) ds[i] = 0.f;
+      }
+      bf16x8 sf[2];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sf[i >> 3][i & 7] = (bf16)ds[i];
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt)
+          qacc[dt] =
+              mfma32x32x16(tr_operand_at(smem, ta, 32 * hh + 16 * c, dt), sf[c], qacc[dt]);
+    }
+  }
+  // The others: only this wave's share of the copies.
+  for (; j < nst; ++j) {
+    wait_vmem();
+    __syncthreads();
+    const i32x4 nk = source(kp, a.k.row, j + 1), nv = source(vp, a.v.row, j + 1);
+#pragma unroll
+    for (int i = 0; i < T::BLK; i += 2) issue(nk, nv, i, lds0 + ((j + 1) & 1) * T::STAGE);
+  }
+  wait_vmem();       // the last stage's empty copies (to LDS) have ended
+  if (KS > 1) {
+    // Add the KS parts' sums in ascending key order: parts 1.. pass theirs through
+    // the stage buffers (16 KB per wave).
+    float* fold = reinterpret_cast<float*>(smem);
+    __syncthreads();   // every wave is done reading the last stage
+    if (ks > 0) {
+      float* mine = fold + ((ks - 1) * T::NQW + wq) * 4096 + lane * 4;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          f32x4 v;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) v[b] = qacc[dt][4 * i + b];
+          *reinterpret_cast<f32x4*>(mine + (4 * dt + i) * 256) = v;
+        }
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int p = 1; p < KS; ++p) {
+      const float* part = fold + ((p - 1) * T::NQW + wq) * 4096 + lane * 4;
+#pragma unroll
+      for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x4 v = *reinterpret_cast<const f32x4*>(part + (4 * dt + i) * 256);
+#pragma unroll
+          for (int b = 0; b < 4; ++b) qacc[dt][4 * i + b] += v[b];
+        }
+    }
+  }
+  if (rw + r32 >= n_rows) return;
+  bf16* op = a.dq.p + (it.q0 + tok) * a.dq.row + (kvh * G + hg) * a.dq.head + 4 * g;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x4 ov;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) ov[b] = (bf16)(qacc[dt][4 * i + b] * kScale);
+      *reinterpret_cast<bf16x4*>(op + 32 * dt + 8 * i) = ov;
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rows_terms(const RowBwdArgs& a, int64_t n, hipStream_t st) {
+  hipLaunchKernelGGL(rows_terms_kernel, dim3((unsigned)(n * a.Hkv)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st) {
+  hipLaunchKernelGGL(rows_dkdv_kernel, dim3((unsigned)(n * a.Hkv)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_dkdv_fold(const RowBwdArgs& a, int64_t n, hipStream_t st) {
+  hipLaunchKernelGGL(rows_dkdv_fold_kernel, dim3((unsigned)(n * 16), (unsigned)a.Hkv), dim3(256), 0,
+                     st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_dq(int ks, const RowBwdArgs& a, int64_t n, hipStream_t st) {
+  const dim3 grid((unsigned)(n * a.Hkv));
+  if (ks == 1) hipLaunchKernelGGL(rows_dq_kernel<1>, grid, dim3(512), 0, st, a);
+  else if (ks == 2) hipLaunchKernelGGL(rows_dq_kernel<2>, grid, dim3(512), 0, st, a);
+  else hipLaunchKernelGGL(rows_dq_kernel<4>, grid, dim3(512), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace upipe
