@@ -76,8 +76,11 @@ int tile_stages(const Lengths& s, int G, int rows, int tile, int causal) {
 }
 
 // Parts into which the keys of a sequence's tiles are cut so that none has more
-// than `most` stages.
-int seq_parts(const Lengths& s, int most) { return s.Lk <= 0 ? 1 : ((s.Lk + 127) / 128 + most - 1) / most; }
+// than `most` stages (if kMostParts suffice).
+int seq_parts(const Lengths& s, int most) {
+  const int stages = (s.Lk + 127) / 128;
+  return std::max(1, std::min(kMostParts, (stages + most - 1) / most));
+}
 
 struct FwdWork {
   RowItem item;
@@ -343,12 +346,16 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   h.fwd_ks = c.ks;
   // Partial rows: [parts][Lq][Hq] of every sequence that is cut.
   std::vector<int64_t> p0;
+  h.parts = 1;
+  for (const Lengths& s : seqs)
+    if (s.Lq > 0) h.parts = std::max(h.parts, seq_parts(s, c.most));
+  const int per_block = h.parts > kSomeParts ? 1 : 16;
   for (const Lengths& s : seqs) {
     const int np = seq_parts(s, c.most);
     p0.push_back(h.part_rows);
     if (np < 2 || s.Lq < 1) continue;
     const int64_t rows = (int64_t)s.Lq * Hq;
-    for (int64_t b = 0; b < (rows + 15) / 16; ++b)
+    for (int64_t b = 0; b < (rows + per_block - 1) / per_block; ++b)
       p->merge.push_back({s.q0, h.part_rows, s.Lq, np, (int32_t)b, 0});
     h.part_rows += np * rows;
   }
@@ -515,6 +522,7 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
       m.lse_head = lse_head;
       m.items = (const MergeItem*)((const char*)plan_dev + h->at_merge);
       m.Hq = Hq;
+      m.parts = h->parts;
       UPIPE_LAUNCH(kRowsMerge, stream, launch_rows_merge(m, h->n_merge, stream));
     }
     return UPIPE_OK;
@@ -607,6 +615,7 @@ namespace {
 
 // How a call over caches is cut: key parts of every row, and of the prefix.
 struct CachePlan {
+  bool few = false;        // at most 32 packed rows of a cache
   int splits = 1;
   int prefix_ks = 1, prefix_parts = 0;
   int64_t rows = 0;        // B * nq * Hq
@@ -622,14 +631,15 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
 
 // The lengths are on the device: the cut goes by the capacity, and a part is the
 // same share of whatever a cache holds.  About four workgroups a CU even out caches of
-// different lengths; a part has four stages of 128 rows at least, as long as the
-// cache is full.
+// different lengths.
 CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv) {
   CachePlan p;
   p.rows = B * nq * Hq;
-  const int64_t G = Hq / Hkv, tiles = (nq * G + 63) / 64, groups = B * Hkv * tiles;
-  const int64_t stages = (cap + 127) / 128;
-  p.splits = (int)std::max<int64_t>(1, std::min((4 * kCUs + groups - 1) / groups, (stages + 3) / 4));
+  const int64_t G = Hq / Hkv;
+  p.few = nq * G <= 32;
+  const int64_t groups = B * Hkv * (p.few ? 1 : (nq * G + 63) / 64);
+  const int64_t least = (cap + 511) / 512;      // parts of 512 rows
+  p.splits = (int)std::max<int64_t>(1, std::min((4 * kCUs + groups - 1) / groups, least));
   if (P > 0) {
     const int64_t rows = B * nq * G, ps = (P + 127) / 128;
     p.prefix_ks = rows > 128 ? 1 : rows > 64 ? 2 : 4;
@@ -717,8 +727,14 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     a.nq = nq;
     a.splits = p.splits;
     a.part0 = p.prefix_parts;
-    const int64_t tiles = ((int64_t)nq * G + 63) / 64;
-    UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, a, tiles * B * p.splits, stream));
+    a.lse_head = nq;
+    if (p.few) {
+      UPIPE_LAUNCH(kRowsFwd, stream, launch_few_rows_fwd(a, B * p.splits, stream));
+    } else {
+      const int64_t tiles = ((int64_t)nq * G + 63) / 64;
+      UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, a, tiles * B * p.splits, stream));
+    }
+    if (cache_parts(p) == 1) return UPIPE_OK;
     RowMergeArgs m{};
     m.part_o = a.part_o;
     m.part_lse = a.part_lse;

@@ -21,7 +21,9 @@ struct RowItem {
   int32_t Lq, Lk;
   int32_t tile, part, parts, pad;
 };
-// 16 rows of a sequence whose parts are merged.
+// 16 rows of a sequence whose parts are merged, or, where some row has more than
+// kSomeParts, one.
+constexpr int kSomeParts = 64, kMostParts = 2048;
 struct MergeItem {
   int64_t q0, p0;
   int32_t Lq, parts, block, pad;
@@ -58,6 +60,7 @@ struct PlanHeader {
   int64_t longest_q, longest_k;
   int32_t n_seq, Hq, Hkv, causal;
   int32_t fwd_ks, dq_ks;               // key parts inside a workgroup
+  int32_t parts;                       // the most of a row
   int32_t n_fwd, n_merge, n_key, n_fold, n_term, n_dq;
   int64_t at_fwd, at_merge, at_key, at_fold, at_term, at_dq;     // byte offsets
 };
@@ -82,6 +85,9 @@ enum RowMode { kRowsPlanned = 0, kRowsCache = 1, kRowsOne = 2 };
 // `blocks` items (of every key/value head).
 hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks, hipStream_t st);
 
+// Caches with at most 32 packed rows (nq G) each: `blocks` as above, parts first.
+hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
+
 struct RowMergeArgs {
   const float *part_o, *part_lse;
   HeadView o;
@@ -89,9 +95,14 @@ struct RowMergeArgs {
   int64_t lse_head;
   const MergeItem* items;    // planned sequences; else all rows of B caches
   int64_t rows;              // B * nq * Hq
-  int Hq, parts, nq;
+  int Hq, nq;
+  int parts;                 // planned: the most of a row
 };
-hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t blocks, hipStream_t st);
+// Whether a workgroup merges one row (else 16): with many parts, or few rows of some.
+inline bool many_parts(int parts, int64_t rows) {
+  return parts > kSomeParts || (parts > 8 && rows < 1024);
+}
+hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t items, hipStream_t st);
 
 // ---- backward (varlen_bwd.hip) ---------------------------------------------
 struct RowBwdArgs {

@@ -44,16 +44,18 @@ __device__ __forceinline__ float tile_probs(const f32x16 (&st)[NT], bf16x8 (&pf)
   return ls;
 }
 
-// One stage (in `buf`) for one wave: the 32 NT keys from key kb on, rows k_part..
-// of the stage.  This lane's row sees the keys up to `lim`, the wave's first row
+// One stage for one wave: the 32 NT keys from key kb on.  k_at and v_at: this lane's
+// place of the first key's chunk g and of its transposing reads of V (common.h); the
+// others are exclusive-ors of them (a register for each would spill).  This lane's row sees the keys up to `lim`, the wave's first row
 // those up to lim_w.  copy_k and copy_v issue the next stage's copies.
 template <int NT, class CopyK, class CopyV>
-__device__ __forceinline__ void fwd_stage(const char* buf, int kb, int k_part, int lane,
+__device__ __forceinline__ void fwd_stage(const char* smem, uint32_t k_at, uint32_t v_at, int kb,
+                                          int lane,
                                           const bf16x8 (&qf)[8], int lim, int lim_w,
                                           f32x16 (&oacc)[4], float& m_ref, float& l_run,
                                           const CopyK& copy_k, const CopyV& copy_v) {
   const float sl2 = 1.4426950408889634f * 0.08838834764831845f;  // log2(e)/sqrt(128)
-  const int r32 = lane & 31, g = lane >> 5;
+  const int g = lane >> 5;
   f32x16 st[NT];
 #pragma unroll
   for (int tt = 0; tt < NT; ++tt)
@@ -63,8 +65,7 @@ __device__ __forceinline__ void fwd_stage(const char* buf, int kb, int k_part, i
   for (int s = 0; s < 8; ++s)
 #pragma unroll
     for (int tt = 0; tt < NT; ++tt)
-      st[tt] = mfma32x32x16(lds_read_b128(buf, swz256(k_part + 32 * tt + r32, 2 * s + g)),
-                            qf[s], st[tt]);
+      st[tt] = mfma32x32x16(lds_read_b128(smem, (k_at ^ (32 * s)) + 8192 * tt), qf[s], st[tt]);
   // Keep six K fragment reads in flight ahead of the MFMAs: left alone,
   // the scheduler reads two, waits for them and multiplies, exposing the
   // LDS latency every two MFMAs.
@@ -116,8 +117,7 @@ __device__ __forceinline__ void fwd_stage(const char* buf, int kb, int k_part, i
   for (int c = 0; c < 2 * NT; ++c)
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
-      oacc[dt] = mfma32x32x16(tr_operand(buf + K_TILE, k_part + 16 * c, 32 * dt, lane),
-                              pf[c >> 1][c & 1], oacc[dt]);
+      oacc[dt] = mfma32x32x16(tr_operand_at(smem, v_at, 16 * c, dt), pf[c >> 1][c & 1], oacc[dt]);
   // Stream the V^T fragments: four (eight transposing reads) ahead, then
   // two reads per MFMA (the default schedule issued bursts of eight
   // reads and waited between them).
@@ -226,6 +226,58 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
   }
 }
 
+// A masked value that is infinite or not a number leaves NaN in the rows of its stage:
+// those are formed again without it.
+__device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_row, const bf16* v,
+                                         int64_t v_row, int key0, int key1, const bf16x8 (&qf)[8],
+                                         int g, f32x16 (&oacc)[4], float& m_ref, float& l) {
+  float z = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) z = fmaf(oacc[dt][i], 0.f, z);
+  z += __shfl_xor(z, 32);
+  if (row_ok && !(z == z))      // both lanes of a row
+    careful_row(k, k_row, v, v_row, key0, key1, qf, g, oacc, m_ref, l);
+}
+
+// A row's result, by the lane pair that holds it: the part's, in fp32, or the row's own.
+__device__ __forceinline__ void write_row(const RowFwdArgs& a, bool part, const RowItem& it,
+                                          int64_t part_rows, int64_t lse_at, int tok, int h, int Hq,
+                                          int g, const f32x16 (&oacc)[4], float m_ref,
+                                          float l_tot) {
+  const bool some = !(l_tot <= 0.f);
+  const float inv = some ? 1.f / l_tot : 0.f;   // no visible key: O = 0
+  const float row_lse = some ? (m_ref + __log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
+  if (part) {
+    const int64_t at = it.p0 + it.part * part_rows + (int64_t)tok * Hq + h;
+    if (g == 0) a.part_lse[at] = row_lse;
+    if (!some) return;           // the merge does not use the row of an empty part
+    float* pp = a.part_o + at * HEAD_DIM + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 ov;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) ov[b] = oacc[dt][4 * i + b] * inv;
+        *reinterpret_cast<f32x4*>(pp + 32 * dt + 8 * i) = ov;
+      }
+    return;
+  }
+  bf16* op = a.o.p + (it.q0 + tok) * a.o.row + h * a.o.head + 4 * g;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x4 ov;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) ov[b] = (bf16)(oacc[dt][4 * i + b] * inv);
+      *reinterpret_cast<bf16x4*>(op + 32 * dt + 8 * i) = ov;
+    }
+  if (g == 0) a.lse[lse_at + h * a.lse_head + tok] = row_lse;
+}
+
 // A workgroup: BQ packed rows of one key/value head against a range of its keys.
 template <int KS, int MODE>
 __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
@@ -238,7 +290,11 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wq = KS == 1 ? w : w % NQW, ks = KS == 1 ? 0 : w / NQW;
   const int r32 = lane & 31, g = lane >> 5;
-  const int kvh = blockIdx.x % a.Hkv, idx = blockIdx.x / a.Hkv, G = a.G, Hq = a.Hkv * G;
+  const int G = a.G, Hq = a.Hkv * G, items = gridDim.x / a.Hkv;
+  // A prefix's parts go round the XCDs, not its heads: an XCD that reads one head of
+  // eight, 256 bytes out of every 2 KB, uses two of its L2's sixteen channels.
+  const int kvh = MODE == kRowsOne ? blockIdx.x / items : blockIdx.x % a.Hkv;
+  const int idx = MODE == kRowsOne ? blockIdx.x % items : blockIdx.x / a.Hkv;
 
   RowItem it;
   int64_t cache = 0, lse_at, part_rows;
@@ -269,7 +325,7 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
   const int n_rows = it.Lq * G, delta = it.Lk - it.Lq;
   const int r0 = it.tile * BQ, rw = r0 + 32 * wq, row = rw + r32;
   const bool row_ok = row < n_rows;
-  const int tok = row / G, hg = row - tok * G;
+  int tok = row / G, hg = row - tok * G;
 
   const uint32_t kb_row = (uint32_t)(a.k.row * 2), vb_row = (uint32_t)(a.v.row * 2);
   const bf16* kp = a.k.p + cache * a.k.batch + it.k0 * a.k.row + kvh * a.k.head;
@@ -334,8 +390,9 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
   float m_ref = -1e30f;
   float l_run = 0.f;         // this lane's partial row sum
 
+  const uint32_t k_lane = swz256(k_part + r32, g), v_lane = K_TILE + k_part * 256 + tr_base(lane);
   for (int j = j0; j < j1; ++j) {
-    const char* buf = smem + (j & 1) * STAGE;
+    const uint32_t boff = (j & 1) * STAGE;
     wait_vmem();
     __syncthreads();   // stage j landed for all waves; stage j-1's buffer is free
     const uint32_t nlds = lds0 + ((j + 1) & 1) * STAGE + 4096 * w;
@@ -345,12 +402,20 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
       copy4_b128(nv, offv, 0, nlds + K_TILE);
       continue;
     }
-    fwd_stage<NT>(buf, j * BKS + k_part, k_part, lane, qf, lim, lim_w, oacc, m_ref, l_run,
+    fwd_stage<NT>(smem, k_lane + boff, v_lane + boff, j * BKS + k_part, lane, qf, lim, lim_w, oacc, m_ref, l_run,
                   [&]() { copy4_b128(nk, offk, 0, nlds); },
                   [&]() { copy4_b128(nv, offv, 0, nlds + K_TILE); });
   }
 
   wait_vmem();       // the last stage's empty copies (to LDS) have ended
+  {
+    // The row's place again: kept through the loop it would spill.
+    int rr = rw;
+    asm volatile("" : "+s"(rr));
+    rr += threadIdx.x & 31;
+    tok = rr / G;
+    hg = rr - tok * G;
+  }
   float l_tot = l_run + __shfl_xor(l_run, 32);
   if (KS > 1) {
     __syncthreads();   // every wave is done reading the last stage, and copying
@@ -359,61 +424,158 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
     if (ks > 0) return;
     fold_in<KS>(smem, wq, lane, oacc, m_ref, l_tot);
   }
-  // A masked value that is infinite or not a number leaves NaN in the rows of its
-  // stage: those are formed again without it.
-  {
-    float z = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z = fmaf(oacc[dt][i], 0.f, z);
-    z += __shfl_xor(z, 32);
-    if (row_ok && !(z == z)) {      // both lanes of a row
-      const int64_t key1 = min((int64_t)lim + 1, (int64_t)j1 * BKS);
-      careful_row(kp, a.k.row, vp, a.v.row, (int64_t)j0 * BKS, key1, qf, g, oacc, m_ref, l_tot);
-    }
-  }
+  mend_row(row_ok, kp, a.k.row, vp, a.v.row, j0 * BKS, min(lim + 1, j1 * BKS), qf, g, oacc, m_ref,
+           l_tot);
   if (!row_ok) return;
-  const bool some = !(l_tot <= 0.f);
-  const float inv = some ? 1.f / l_tot : 0.f;   // no visible key: O = 0
-  const float row_lse = some ? (m_ref + __log2f(l_tot)) * 0.6931471805599453f : -INFINITY;
-  const int h = kvh * G + hg;
-  if (MODE != kRowsPlanned || it.parts > 1) {
-    const int64_t at = it.p0 + it.part * part_rows + (int64_t)tok * Hq + h;
-    if (g == 0) a.part_lse[at] = row_lse;
-    if (!some) return;           // the merge does not read the row of an empty part
-    float* pp = a.part_o + at * HEAD_DIM + 4 * g;
+  write_row(a, MODE == kRowsOne || (MODE == kRowsCache ? a.splits + a.part0 : it.parts) > 1, it, part_rows, lse_at, tok, kvh * G + hg, Hq, g,
+            oacc, m_ref, l_tot);
+}
+
+// Up to 32 packed rows of one cache and key/value head: a wave takes every NW-th 32-key
+// tile of the workgroup's part, each by itself: it copies its tile's K and V rows into
+// its own LDS, two tiles deep, waits for its own copies and meets the other waves only at
+// the end.  No barrier in the walk, and two workgroups a CU, so that one's start and end
+// hide behind the other's stream.
+constexpr int kFewWaves = 2;
+constexpr int kFewTile = 32 * HEAD_DIM * 2;        // K or V rows of a tile: 8 KB
+constexpr int kFewLds = kFewWaves * 4 * kFewTile;
+
+__global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[kFewLds];
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r32 = lane & 31, g = lane >> 5;
+  const int kvh = blockIdx.x % a.Hkv, idx = blockIdx.x / a.Hkv, G = a.G, Hq = a.Hkv * G;
+  const int b = idx / a.splits;
+  RowItem it{};
+  it.part = idx % a.splits;
+  it.q0 = (int64_t)b * a.nq;
+  it.p0 = it.q0 * Hq;
+  const int Lk = (int)min(max((int64_t)a.lens[b], (int64_t)0), a.cap);
+  const int n_rows = a.nq * G, delta = Lk - a.nq;
+  const bool row_ok = r32 < n_rows;
+  const int tok = r32 / G, hg = r32 - tok * G;
+
+  const bf16* kp = a.k.p + b * a.k.batch + kvh * a.k.head;
+  const bf16* vp = a.v.p + b * a.v.batch + kvh * a.v.head;
+  const uint32_t k_row = (uint32_t)(a.k.row * 2), v_row = (uint32_t)(a.v.row * 2);
+  // Four blocks of four rows; the other four lie 16 rows on, swizzled alike.
+  uint32_t offk[4], offv[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 4 * i + (lane >> 4);
+    offk[i] = r * k_row + ((uint32_t)((lane & 15) ^ r) << 4);
+    offv[i] = r * v_row + (((lane & 15) ^ tsw(r)) << 4);
+  }
+  // Every row's keys end by Lk; this part's tiles, and this wave's of them.
+  const int tiles = (Lk + 31) / 32, per = (tiles + a.splits - 1) / a.splits;
+  const int t0 = min(tiles, per * it.part), t1 = min(tiles, t0 + per);
+  const uint32_t lds = lds_address(smem) + w * 4 * kFewTile;
+  auto copy = [&](int t, uint32_t to) {
+    // 16 rows from row r on, those past the last key as zeros
+    auto source = [&](const bf16* p, int64_t row, int r) {
+      const int n = t < t1 ? min(16, Lk - r) : 0;
+      return rsrc_words(p + r * row, n > 0 ? (uint32_t)((n - 1) * (int)row + HEAD_DIM) * 2 : 0);
+    };
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 32 * t + 16 * half;
+      copy4_b128(source(kp, a.k.row, r), offk, 0, to + 4096 * half);
+      copy4_b128(source(vp, a.v.row, r), offv, 0, to + kFewTile + 4096 * half);
+    }
+  };
+  copy(t0 + w, lds);
+  copy(t0 + w + kFewWaves, lds + 2 * kFewTile);
+
+  bf16x8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) qf[s][e] = (bf16)0.f;
+  if (row_ok) {
+    const bf16* qp = a.q.p + (it.q0 + tok) * a.q.row + (kvh * G + hg) * a.q.head + 8 * g;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s);
+  }
+  f32x16 oacc[4];
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
+  float m_ref = -1e30f, l_run = 0.f;
+  const int lim = min(tok + delta, Lk - 1), lim_w = delta;      // of token 0
+  const uint32_t k_lane = swz256(r32, g), v_lane = kFewTile + tr_base(lane);
+  // The queries are here before the walk (the compiler waits for them and, with them, for
+  // the first copies): within it, it would wait for every copy.
+#pragma unroll
+  for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
+  for (int t = t0 + w, n = 0; t < t1; t += kFewWaves, ++n) {
+    const uint32_t boff = (w * 4 + 2 * (n & 1)) * kFewTile;
+    // This tile's 16 copies have landed; the next one's may be under way.
+    asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
+    fwd_stage<1>(smem, k_lane + boff, v_lane + boff, 32 * t, lane, qf, lim, lim_w, oacc, m_ref, l_run,
+                 []() {}, []() {});
+    // Every read of the tile is done: its place takes the copies of the next but one.
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    copy(t + 2 * kFewWaves, lds_address(smem) + boff);
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the last, empty copies have ended
+  float l_tot = l_run + __shfl_xor(l_run, 32);
+  // The waves' parts folded in fp32, in their order, through LDS.
+  float* fold = reinterpret_cast<float*>(smem);
+  __syncthreads();
+  if (w > 0) {
+    float* mine = fold + (w - 1) * (4096 + 128) + lane * 4;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        f32x4 ov;
+        f32x4 v;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) ov[b] = oacc[dt][4 * i + b] * inv;
-        *reinterpret_cast<f32x4*>(pp + 32 * dt + 8 * i) = ov;
+        for (int e = 0; e < 4; ++e) v[e] = oacc[dt][4 * i + e];
+        *reinterpret_cast<f32x4*>(mine + (4 * dt + i) * 256) = v;
       }
-    return;
+    fold[(w - 1) * (4096 + 128) + 4096 + lane] = m_ref;
+    fold[(w - 1) * (4096 + 128) + 4096 + 64 + lane] = l_tot;
   }
-  bf16* op = a.o.p + (it.q0 + tok) * a.o.row + h * a.o.head + 4 * g;
+  __syncthreads();
+  if (w > 0) return;
 #pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
+  for (int p = 0; p < kFewWaves - 1; ++p) {
+    const float* part = fold + p * (4096 + 128);
+    const float m_p = part[4096 + lane], l_p = part[4096 + 64 + lane];
+    const float m_new = fmaxf(m_ref, m_p);
+    const float a0 = fast_exp2(m_ref - m_new), a1 = fast_exp2(m_p - m_new);
+    m_ref = m_new;
+    l_tot = l_tot * a0 + l_p * a1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      bf16x4 ov;
+    for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) ov[b] = (bf16)(oacc[dt][4 * i + b] * inv);
-      *reinterpret_cast<bf16x4*>(op + 32 * dt + 8 * i) = ov;
-    }
-  if (g == 0) a.lse[lse_at + h * a.lse_head + tok] = row_lse;
+      for (int i = 0; i < 4; ++i) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(part + (4 * dt + i) * 256 + lane * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          oacc[dt][4 * i + e] = oacc[dt][4 * i + e] * a0 + v[e] * a1;
+      }
+  }
+  mend_row(row_ok, kp, a.k.row, vp, a.v.row, 32 * t0, min(lim + 1, 32 * t1), qf, g, oacc, m_ref, l_tot);
+  if (!row_ok) return;
+  it.part += a.part0;
+  write_row(a, a.splits + a.part0 > 1, it, (int64_t)a.B * a.nq * Hq, it.p0, tok, kvh * G + hg, Hq, g,
+            oacc, m_ref, l_tot);
 }
 
 // The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
-// rounding.  Sixteen lanes a row, GP groups of them to share many parts.
+// rounding.  Sixteen lanes a row, GP groups of them to share many parts: first the
+// weights of all parts, then their outputs, several loads under way at a time (one
+// after the other 256 parts of 8 rows took 17 us, twice what forming them did).
 template <int GP, bool PLANNED>
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
-  __shared__ float sh[GP > 1 ? GP : 1][HEAD_DIM + 2];
+  constexpr int ROWS = 16 / GP;                       // of a workgroup
+  __shared__ float weights[ROWS][GP > 1 ? kMostParts : kSomeParts];
+  __shared__ float sh[GP][HEAD_DIM], red[8];
   const int c = threadIdx.x & 15, grp = threadIdx.x >> 4;
-  const int gp = GP > 1 ? grp : 0;
+  const int gp = GP > 1 ? grp : 0, lr = GP > 1 ? 0 : grp;
   int64_t r, q0 = 0, p0 = 0, rows = a.rows;
   int parts = a.parts;
   if (PLANNED) {
@@ -422,56 +584,89 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
     p0 = it.p0;
     rows = (int64_t)it.Lq * a.Hq;
     parts = it.parts;
-    r = (int64_t)it.block * 16 + grp;
+    r = (int64_t)it.block * ROWS + lr;
   } else {
-    r = (int64_t)blockIdx.x * (16 / GP) + (GP > 1 ? 0 : grp);
+    r = (int64_t)blockIdx.x * ROWS + lr;
   }
-  if (r >= rows) return;         // GP > 1: a whole workgroup
+  if (r >= rows) return;         // GP > 1: none or all of a workgroup
   const float* pl = a.part_lse + p0 + r;
-  float m = -INFINITY;
-  for (int i = gp; i < parts; i += GP) m = fmaxf(m, pl[i * rows]);
-  // (a NaN is passed over by fmaxf and comes in with its weight)
-  float l = 0.f, acc[8];
+  float m = -INFINITY, l = 0.f;
+  if (GP == 1) {
+    float v[kSomeParts / 16];
+#pragma unroll
+    for (int u = 0; u < kSomeParts / 16; ++u) {
+      v[u] = c + 16 * u < parts ? pl[(c + 16 * u) * rows] : -INFINITY;
+      m = fmaxf(m, v[u]);
+    }
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    // (a NaN is passed over by fmaxf and comes in with its weight)
+#pragma unroll
+    for (int u = 0; u < kSomeParts / 16; ++u) {
+      const float wt = v[u] == -INFINITY ? 0.f : v[u] == m ? 1.f : __expf(v[u] - m);
+      weights[lr][c + 16 * u] = wt;
+      l += wt;
+    }
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) l += __shfl_xor(l, off);
+    __builtin_amdgcn_wave_barrier();
+  } else {
+    for (int i = threadIdx.x; i < parts; i += 256) {
+      const float v = pl[i * rows];
+      weights[0][i] = v;
+      m = fmaxf(m, v);
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    for (int i = threadIdx.x; i < parts; i += 256) {
+      const float v = weights[0][i];
+      const float wt = v == -INFINITY ? 0.f : v == m ? 1.f : __expf(v - m);
+      weights[0][i] = wt;
+      l += wt;
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
+    if ((threadIdx.x & 63) == 0) red[4 + (threadIdx.x >> 6)] = l;
+    __syncthreads();
+    l = (red[4] + red[5]) + (red[6] + red[7]);
+  }
+  float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
   const float* po = a.part_o + (p0 + r) * HEAD_DIM + 8 * c;
-#pragma unroll 4
-  for (int i = gp; i < parts; i += GP) {
-    const float li = pl[i * rows];
-    if (li == -INFINITY) continue;       // an empty part: its row is not written
-    const float wt = li == m ? 1.f : __expf(li - m);
-    const float* p = po + i * rows * HEAD_DIM;
-    const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
-    l += wt;
+  constexpr int U = 4;
+  for (int i0 = gp; i0 < parts; i0 += U * GP) {
+    f32x4 lo[U], hi[U];
+    float wt[U];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      acc[e] = fmaf(wt, lo[e], acc[e]);
-      acc[4 + e] = fmaf(wt, hi[e], acc[4 + e]);
+    for (int u = 0; u < U; ++u) {
+      const int i = min(i0 + u * GP, parts - 1);
+      const float* p = po + i * rows * HEAD_DIM;
+      lo[u] = *reinterpret_cast<const f32x4*>(p);
+      hi[u] = *reinterpret_cast<const f32x4*>(p + 4);
+      wt[u] = i0 + u * GP < parts ? weights[lr][i] : 0.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool empty = wt[u] == 0.f;       // an empty part's row is not written
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[e] = fmaf(wt[u], empty ? 0.f : lo[u][e], acc[e]);
+        acc[4 + e] = fmaf(wt[u], empty ? 0.f : hi[u][e], acc[4 + e]);
+      }
     }
   }
   if (GP > 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sh[gp][8 * c + e] = acc[e];
-    if (c == 0) {
-      sh[gp][HEAD_DIM] = m;
-      sh[gp][HEAD_DIM + 1] = l;
-    }
     __syncthreads();
     if (gp > 0) return;
-    float mm = m;
-    for (int i = 1; i < GP; ++i) mm = fmaxf(mm, sh[i][HEAD_DIM]);
-    l = 0.f;
+    for (int i = 1; i < GP; ++i)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-    for (int i = 0; i < GP; ++i) {
-      const float mi = sh[i][HEAD_DIM], ln = sh[i][HEAD_DIM + 1];
-      if (mi == -INFINITY && ln == 0.f) continue;
-      const float wt = mi == mm ? 1.f : __expf(mi - mm);
-      l = fmaf(wt, ln, l);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = fmaf(wt, sh[i][8 * c + e], acc[e]);
-    }
-    m = mm;
+      for (int e = 0; e < 8; ++e) acc[e] += sh[i][8 * c + e];
   }
   const bool some = !(l <= 0.f);
   const int64_t tok = r / a.Hq;
@@ -507,15 +702,24 @@ hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks
   return hipGetLastError();
 }
 
-hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t blocks, hipStream_t st) {
+hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
+  hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)(blocks * a.Hkv)), dim3(64 * kFewWaves), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t items, hipStream_t st) {
+  const bool many = a.items != nullptr ? a.parts > kSomeParts : many_parts(a.parts, a.rows);
+  const int64_t blocks = a.items != nullptr ? items : many ? a.rows : (a.rows + 15) / 16;
+#define UPIPE_MERGE(GP, P) \
+  hipLaunchKernelGGL((rows_merge_kernel<GP, P>), dim3((unsigned)blocks), dim3(256), 0, st, a)
   if (a.items != nullptr) {
-    hipLaunchKernelGGL((rows_merge_kernel<1, true>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  } else if (a.parts > 16) {
-    hipLaunchKernelGGL((rows_merge_kernel<16, false>), dim3((unsigned)a.rows), dim3(256), 0, st, a);
+    if (many) UPIPE_MERGE(16, true);
+    else UPIPE_MERGE(1, true);
   } else {
-    hipLaunchKernelGGL((rows_merge_kernel<1, false>), dim3((unsigned)((a.rows + 15) / 16)), dim3(256),
-                       0, st, a);
+    if (many) UPIPE_MERGE(16, false);
+    else UPIPE_MERGE(1, false);
   }
+#undef UPIPE_MERGE
   return hipGetLastError();
 }
 
