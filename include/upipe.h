@@ -323,8 +323,8 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
  *   q, k, v, o, lse   as given to and left by upipe_attn_fwd_varlen
  *   dout              upstream gradient of o, rows [.., Hq, d]
  *   dq, dk, dv        out: rows [.., Hq, d], [.., Hkv, d] (summed over each group's
- *                     query heads); dq may be q or dout.  They may be columns of one
- *                     buffer, as q, k, v of a projection are.
+ *                     query heads).  They may be columns of one buffer, as q, k, v
+ *                     of a projection are.
  * Rows of 128 / G tokens (G = Hq / Hkv) of q and of dout, all heads of a group, must
  * span less than 2^30 bytes (UPIPE_ERR_UNSUPPORTED).  P and dS are rounded to bf16 for
  * their products, every sum is fp32 in a fixed order.  A masked pair's infinite or NaN

@@ -248,7 +248,7 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
 constexpr double kDqStage[3] = {2.5, 2.8, 1.6}, kDqFixed = 4.0;
 
 struct DqWork {
-  DqItem item;
+  TileItem item;
   int stages;
 };
 
@@ -308,10 +308,10 @@ struct Plan {
   PlanHeader h{};
   std::vector<RowItem> fwd;
   std::vector<MergeItem> merge;
-  std::vector<TermItem> terms;
+  std::vector<TileItem> terms;
   std::vector<KeyItem> keys;
   std::vector<FoldItem> folds;
-  std::vector<DqItem> dqs;
+  std::vector<TileItem> dqs;
 };
 
 template <class T>
@@ -367,7 +367,7 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   const int tpt = tile_tokens(G);
   for (const Lengths& s : seqs) {
     for (int t = 0; t < (s.Lq + tpt - 1) / tpt; ++t)
-      p->terms.push_back({s.q0, h.term_rows, s.Lq, s.Lk, t, 0});
+      p->terms.push_back({s.q0, s.k0, h.term_rows, s.Lq, s.Lk, t, 0});
     h.term_rows += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
   }
   key_work(seqs, G, causal, choose_segment(seqs, G, Hkv, causal), &p->keys, &p->folds, &h.slots);
@@ -555,9 +555,8 @@ int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
     if ((Tq > 0 && !heads_distinct(dq, Tq, Hq)) ||
         (Tk > 0 && (!heads_distinct(dk, Tk, Hkv) || !heads_distinct(dv, Tk, Hkv))))
       return UPIPE_ERR_INVALID_ARG;
-    // dq may be q or dout: its kernel comes last, and reads a row before it writes it.
     for (int i = 0; i < 3; ++i)
-      if ((!(i != 1 && heads_same(dq, *rq[i])) && !apart(dq, Tq, Hq, *rq[i], Tq, Hq)) ||
+      if (!apart(dq, Tq, Hq, *rq[i], Tq, Hq) ||
           !apart(dk, Tk, Hkv, *rq[i], Tq, Hq) || !apart(dv, Tk, Hkv, *rq[i], Tq, Hq))
         return UPIPE_ERR_INVALID_ARG;
     for (int i = 0; i < 2; ++i)
@@ -588,18 +587,18 @@ int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
     a.lse_c = a.D + Hkv * h->term_rows;
     a.sums = (float*)((char*)ws + sums_at(*h));
     a.slots = h->slots;
-    a.terms = (const TermItem*)(dev + h->at_term);
+    a.terms = (const TileItem*)(dev + h->at_term);
     a.keys = (const KeyItem*)(dev + h->at_key);
     a.folds = (const FoldItem*)(dev + h->at_fold);
-    a.dqs = (const DqItem*)(dev + h->at_dq);
+    a.dqs = (const TileItem*)(dev + h->at_dq);
     a.Hkv = Hkv;
     a.G = G;
     a.causal = h->causal;
     if (h->n_term > 0) UPIPE_LAUNCH(kRowsTerms, stream, launch_rows_terms(a, h->n_term, stream));
+    if (h->n_dq > 0) UPIPE_LAUNCH(kRowsDq, stream, launch_rows_dq(h->dq_ks, a, h->n_dq, stream));
     if (h->n_key > 0) UPIPE_LAUNCH(kRowsDkdv, stream, launch_rows_dkdv(a, h->n_key, stream));
     if (h->n_fold > 0)
       UPIPE_LAUNCH(kRowsDkdvFold, stream, launch_rows_dkdv_fold(a, h->n_fold, stream));
-    if (h->n_dq > 0) UPIPE_LAUNCH(kRowsDq, stream, launch_rows_dq(h->dq_ks, a, h->n_dq, stream));
     return UPIPE_OK;
   } catch (...) {
     return UPIPE_ERR_HIP;

@@ -40,12 +40,8 @@ struct FoldItem {
   int64_t k0;
   int32_t Lk, kb, slot, n;
 };
-// A tile of row terms: query tile `tile` of a sequence.
-struct TermItem {
-  int64_t q0, r0;
-  int32_t Lq, Lk, tile, pad;
-};
-struct DqItem {
+// Tile `tile` of a sequence's packed rows: of 128 for the row terms, of dQ's own size.
+struct TileItem {
   int64_t q0, k0, r0;
   int32_t Lq, Lk, tile, pad;
 };
@@ -115,10 +111,10 @@ struct RowBwdArgs {
   int64_t term_rows;
   float* sums;               // [Hkv][slots][2][128][128] sums of segments
   int64_t slots;
-  const TermItem* terms;
+  const TileItem* terms;
   const KeyItem* keys;
   const FoldItem* folds;
-  const DqItem* dqs;
+  const TileItem* dqs;
   int Hkv, G, causal;
 };
 // n items of every key/value head.

@@ -8,10 +8,10 @@
 // a key/value group are packed (varlen.h), so dK and dV sum over the group's heads by
 // walking its rows.  No atomics: every sum has a fixed order.
 //   terms: D and -sqrt(d) lse of the packed rows, in tiles of 128
+//   dq:    a workgroup owns 256, 128 or 64 packed rows and walks stages of keys
 //   dkdv:  a workgroup owns 128 keys of one key/value head and walks the tiles of
 //          rows that see them, from the last one down; long walks are cut into
 //          segments side by side, whose sums are added in their order
-//   dq:    a workgroup owns 256, 128 or 64 packed rows and walks stages of keys
 // The products of a tile are those of the backward over equal lengths
 // (attn_bwd_tile.h).
 #include "attn_bwd_tile.h"
@@ -25,7 +25,7 @@ namespace {
 // every pair of theirs is masked, and zeros keep what is masked finite.
 __global__ __launch_bounds__(256) void rows_terms_kernel(RowBwdArgs a) {
   const int kvh = blockIdx.x / 4 % a.Hkv;
-  const TermItem it = a.terms[blockIdx.x / 4 / a.Hkv];
+  const TileItem it = a.terms[blockIdx.x / 4 / a.Hkv];
   const int c = threadIdx.x & 15, G = a.G, tpt = tile_tokens(G);
   const int64_t out = kvh * a.term_rows + it.r0 + it.tile * 128;
 #pragma unroll
@@ -296,6 +296,12 @@ struct DqTile {
   static constexpr int BLK = T / 1024 / 8;          // 1 KB blocks per wave per tensor
 };
 constexpr int DQ_LA = 4;     // K/V fragment reads kept in flight
+// D of the rows that see no more keys than these, one block of products, comes from
+// the weights themselves, and dK/dV after this kernel uses it: o carries half a step of
+// bf16 and the steps of the weights that formed it, and where few keys share the weight
+// dP - D cancels to little more than that.  Documents of 1 to 700 tokens: dQ and dK
+// 2.4e-3 off instead of 2.6e-3 (2.3e-3 are the roundings of dS and of the result).
+constexpr int kFewKeys = 32;
 
 template <int KS>
 __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
@@ -307,7 +313,7 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
   const int wq = KS == 1 ? w : w % T::NQW, ks = KS == 1 ? 0 : w / T::NQW;
   const int r32 = lane & 31, g = lane >> 5;
   const int kvh = blockIdx.x % a.Hkv, G = a.G;
-  const DqItem it = a.dqs[blockIdx.x / a.Hkv];
+  const TileItem it = a.dqs[blockIdx.x / a.Hkv];
   const int n_rows = it.Lq * G, delta = it.Lk - it.Lq;
   const int r0 = it.tile * T::BQ, rw = r0 + 32 * wq;
   const int row = min(rw + r32, n_rows - 1);     // rows past the last compute on it
@@ -343,6 +349,9 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
     for (int i = 0; i < T::BLK; i += 2) issue(rk, rv, i, lds0);
   }
 
+  auto term_of = [&](int tpt) {
+    return kvh * a.term_rows + it.r0 + (int64_t)(tok / tpt) * 128 + (tok % tpt) * G + hg;
+  };
   bf16x8 qf[8], df[8];
   float nlse, Dq;   // nlse = -sqrt(d) lse: the score accumulator's seed
   {
@@ -354,10 +363,8 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
       qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s);
       df[s] = *reinterpret_cast<const bf16x8*>(dp + 16 * s);
     }
-    const int64_t term =
-        kvh * a.term_rows + it.r0 + (int64_t)(tok / tpt) * 128 + (tok % tpt) * G + hg;
-    nlse = a.lse_c[term];
-    Dq = a.D[term];
+    nlse = a.lse_c[term_of(tpt)];
+    Dq = a.D[term_of(tpt)];
   }
 
   f32x16 qacc[4];
@@ -407,6 +414,19 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
       // The next tile's copies go out behind the products they can hide behind.
       if (hh == 0) issue(nk, nv, 0, nlds);
       if (T::BLK > 2 && hh == T::NH - 1) issue(nk, nv, 2, nlds);
+      if (hh == 0 && kb == 0 && lim_w < kFewKeys) {
+        // All that the first rows see are these keys: D = sum_j P_ij dP_ij.
+        float d = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (8 * (i >> 2) + 4 * g + (i & 3) <= lim)
+            d = fmaf(fast_exp2(sacc[i] * kSl2), pacc[i], d);
+        d += __shfl_xor(d, 32);
+        if (lim >= 0 && lim < kFewKeys) {
+          Dq = d;
+          if (g == 0 && rw + r32 < n_rows) a.D[term_of(tile_tokens(G))] = d;
+        }
+      }
       float ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) ds[i] = fast_exp2(sacc[i] * kSl2) * (pacc[i] - Dq);

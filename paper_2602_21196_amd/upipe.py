@@ -624,40 +624,38 @@ def _rows(t, name, shape=None):
     torch = _torch()
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [T,H,d], got {tuple(t.shape)}")
-    if shape is not None:
-        _shape(t, shape, name)
-    T, H, d = t.shape
-    if d > 1 and t.stride(2) != 1:
-        raise ValueError(f"{name} must have dense rows, got strides {t.stride()}")
-    head = t.stride(1) if H > 1 else d
-    row = t.stride(0) if T > 1 else H * head
-    return upipe_heads(t.data_ptr(), row, head)
+    size, stride = t.shape, t.stride()
+    if len(size) != 3:
+        raise ValueError(f"{name} must be [T,H,d], got {tuple(size)}")
+    if shape is not None and size != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(size)}")
+    T, H, d = size
+    if d > 1 and stride[2] != 1:
+        raise ValueError(f"{name} must have dense rows, got strides {stride}")
+    head = stride[1] if H > 1 else d
+    return upipe_heads(t.data_ptr(), stride[0] if T > 1 else H * head, head)
 
 
-class _Call:
-    """The device of a call's tensors, made the current one around it, and its
-    current stream; every tensor of the call has to be on it."""
-
-    def __init__(self, **tensors):
-        devices = {t.device for t in tensors.values() if t is not None}
-        if len(devices) != 1:
+def _call(fn, args, **tensors):
+    """lib().fn(*args, stream) on the current stream of the tensors' device, made the
+    current one; all of them have to be on it."""
+    it = iter(tensors.values())
+    dev = next(it).get_device()
+    for t in it:
+        if t is not None and t.get_device() != dev:
             raise ValueError("tensors on different devices: " + ", ".join(
                 f"{n} on {t.device}" for n, t in tensors.items() if t is not None))
-        self.device = devices.pop()
-        self._at = _torch().cuda.device(self.device)
-
-    def __enter__(self):
-        self._at.__enter__()
-        return _stream()
-
-    def __exit__(self, *exc):
-        return self._at.__exit__(*exc)
+    cuda = _torch().cuda
+    if cuda.current_device() == dev:
+        st = getattr(lib(), fn)(*args, cuda.current_stream().cuda_stream)
+    else:
+        with cuda.device(dev):
+            st = getattr(lib(), fn)(*args, cuda.current_stream().cuda_stream)
+    _check(fn, st)
 
 
 def _workspace(ws, need, device, fn):
@@ -704,10 +702,10 @@ def qk_norm_rope(q, k, wq, wk, positions, base, eps=1e-6, out=None):
     q, k and out = (q', k') may be strided views with dense rows; out may be (q, k)."""
     T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
     yq, yk = _pair_out(out, (tuple(q.shape), tuple(k.shape)), q.device, ("q_out", "k_out"))
-    with _Call(q=q, k=k, wq=wq, wk=wk, positions=positions, q_out=yq, k_out=yk) as stream:
-        st = upipe_qk_norm_rope(vq, vk, *rest, _rows(yq, "q_out"), _rows(yk, "k_out"), T, Hq, Hkv,
-                                q.shape[2], float(base), float(eps), stream)
-    _check("upipe_qk_norm_rope", st)
+    _call("upipe_qk_norm_rope",
+          (vq, vk, *rest, _rows(yq, "q_out"), _rows(yk, "k_out"), T, Hq, Hkv, q.shape[2],
+           float(base), float(eps)),
+          q=q, k=k, wq=wq, wk=wk, positions=positions, q_out=yq, k_out=yk)
     return yq, yk
 
 
@@ -721,12 +719,12 @@ def qk_norm_rope_bwd(q, k, wq, wk, positions, base, dq_out, dk_out, eps=1e-6, ou
     dwq, dwk = torch.empty_like(wq), torch.empty_like(wk)
     ws = _workspace(ws, upipe_qk_norm_rope_bwd_workspace_size(T, Hq, Hkv, q.shape[2]), q.device,
                     "upipe_qk_norm_rope_bwd_workspace_size")
-    with _Call(q=q, k=k, wq=wq, wk=wk, positions=positions, dq_out=dq_out, dk_out=dk_out, dq=dq,
-               dk=dk, ws=ws) as stream:
-        st = upipe_qk_norm_rope_bwd(vq, vk, *rest, vdq, vdk, _rows(dq, "dq"), _rows(dk, "dk"),
-                                    dwq.data_ptr(), dwk.data_ptr(), T, Hq, Hkv, q.shape[2],
-                                    float(base), float(eps), ws.data_ptr(), ws.numel(), stream)
-    _check("upipe_qk_norm_rope_bwd", st)
+    _call("upipe_qk_norm_rope_bwd",
+          (vq, vk, *rest, vdq, vdk, _rows(dq, "dq"), _rows(dk, "dk"), dwq.data_ptr(),
+           dwk.data_ptr(), T, Hq, Hkv, q.shape[2], float(base), float(eps), ws.data_ptr(),
+           ws.numel()),
+          q=q, k=k, wq=wq, wk=wk, positions=positions, dq_out=dq_out, dk_out=dk_out, dq=dq, dk=dk,
+          ws=ws)
     return dq, dk, dwq, dwk
 
 
@@ -803,17 +801,17 @@ def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
     else:
         o, lse = out
     ws = _workspace(ws, plan.fwd_workspace, q.device, "upipe_attn_fwd_varlen_workspace_size")
-    with _Call(q=q, k=k, v=v, o=o, lse=lse, plan=plan.dev, ws=ws) as stream:
-        st = upipe_attn_fwd_varlen(*views, _packed(o, "o", Tq, plan.Hq), *_packed_lse(lse, q, plan),
-                                   plan.host, plan.dev.data_ptr(), ws.data_ptr(), ws.numel(), stream)
-    _check("upipe_attn_fwd_varlen", st)
+    _call("upipe_attn_fwd_varlen",
+          (*views, _packed(o, "o", Tq, plan.Hq), *_packed_lse(lse, q, plan), plan.host,
+           plan.dev.data_ptr(), ws.data_ptr(), ws.numel()),
+          q=q, k=k, v=v, o=o, lse=lse, plan=plan.dev, ws=ws)
     return o, lse
 
 
 def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     """(dq, dk, dv) of the packed q, k, v, with o and lse of attn_fwd_varlen and the
     same plan.  Rows behind the last sequence are left as they are in out = (dq, dk, dv),
-    0 in new tensors; dq may be q or dout."""
+    0 in new tensors."""
     torch = _torch()
     Tq, Tk = plan.total_q, plan.total_k
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
@@ -827,21 +825,29 @@ def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     grads = (_packed(dout, "dout", Tq, plan.Hq), _packed(dq, "dq", Tq, plan.Hq),
              _packed(dk, "dk", Tk, plan.Hkv), _packed(dv, "dv", Tk, plan.Hkv))
     ws = _workspace(ws, plan.bwd_workspace, q.device, "upipe_attn_bwd_varlen_workspace_size")
-    with _Call(q=q, k=k, v=v, o=o, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, plan=plan.dev,
-               ws=ws) as stream:
-        st = upipe_attn_bwd_varlen(*views, *_packed_lse(lse, q, plan), *grads, plan.host,
-                                   plan.dev.data_ptr(), ws.data_ptr(), ws.numel(), stream)
-    _check("upipe_attn_bwd_varlen", st)
+    _call("upipe_attn_bwd_varlen",
+          (*views, *_packed_lse(lse, q, plan), *grads, plan.host, plan.dev.data_ptr(),
+           ws.data_ptr(), ws.numel()),
+          q=q, k=k, v=v, o=o, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, plan=plan.dev, ws=ws)
     return dq, dk, dv
 
 
 def _cache(t, name, B, Hkv):
     """(upipe_heads of one cache, elements from one to the next) of [B, cap, Hkv, d]."""
-    if not isinstance(t, _torch().Tensor) or t.dim() != 4:
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.dim() != 4:
         raise ValueError(f"{name} must be [B,cap,Hkv,d]")
-    _shape(t, (B, t.shape[1], Hkv, 128), name)
-    v = _rows(t[0], name)
-    return v, t.stride(0) if B > 1 else 0
+    if t.dtype is not torch.bfloat16:
+        raise TypeError(f"{name} must be {torch.bfloat16}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    cap = t.shape[1]
+    _shape(t, (B, cap, Hkv, 128), name)
+    step, row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name} must have dense rows, got strides {t.stride()}")
+    head = head if Hkv > 1 else 128
+    return upipe_heads(t.data_ptr(), row if cap > 1 else Hkv * head, head), step if B > 1 else 0
 
 
 def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=None, ws=None):
@@ -879,12 +885,12 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
         _shape(lse, (B, Hq, nq), "lse")
     need = upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d)
     ws = _workspace(ws, need, q.device, "upipe_attn_decode_workspace_size")
-    with _Call(q=q, k_cache=k_cache, v_cache=v_cache, lens=lens, k_prefix=k_prefix,
-               v_prefix=v_prefix, o=o, lse=lse, ws=ws) as stream:
-        st = upipe_attn_decode(vq, vk, k_step, vv, v_step, _ptr(lens, torch.int32, "lens"), vkp, vvp,
-                               _rows(_flat_tokens(o, "o"), "o"), _ptr(lse, torch.float32, "lse"),
-                               B, nq, cap, P, Hq, Hkv, d, ws.data_ptr(), ws.numel(), stream)
-    _check("upipe_attn_decode", st)
+    _call("upipe_attn_decode",
+          (vq, vk, k_step, vv, v_step, _ptr(lens, torch.int32, "lens"), vkp, vvp,
+           _rows(_flat_tokens(o, "o"), "o"), _ptr(lse, torch.float32, "lse"), B, nq, cap, P, Hq,
+           Hkv, d, ws.data_ptr(), ws.numel()),
+          q=q, k_cache=k_cache, v_cache=v_cache, lens=lens, k_prefix=k_prefix, v_prefix=v_prefix,
+          o=o, lse=lse, ws=ws)
     return o, lse
 
 

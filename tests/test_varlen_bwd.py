@@ -76,15 +76,11 @@ def test_layouts_places_and_rows_behind_the_last():
         assert torch.equal(buf[:n], want)
         new = upipe.attn_bwd_varlen(q, k, v, o, lse, dout, plan)
         assert all(bool((t[n:] == 0).all()) for t in new)
-        # dq over the upstream gradient, and over the queries
+        # what the workspace held before does not matter
         ws = upipe.workspace(plan.bwd_workspace, DEV).fill_(255)
-        for over in (dout, q):
-            place = over.clone(memory_format=torch.preserve_format)
-            args = [q, k, v, o, lse, dout]
-            args[5 if over is dout else 0] = place
-            upipe.attn_bwd_varlen(*args, plan, out=(place, dk, dv), ws=ws)
-            torch.cuda.synchronize()
-            assert torch.equal(place[:n], want[:, :Hq]), (name, over is dout)
+        again = upipe.attn_bwd_varlen(q, k, v, o, lse, dout, plan, ws=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(torch.cat(again, 1)[:n], want)
 
 
 @pytest.mark.gpu
@@ -194,9 +190,8 @@ def test_refusals():
                 dict(dq=_heads(6 * FAKE, head=0)), dict(dk=_heads(7 * FAKE, 64)), dict(dv=_heads(0)),
                 dict(dq=_heads(4 * FAKE)), dict(dq=_heads(2 * FAKE)), dict(dk=_heads(2 * FAKE, D)),
                 dict(dv=_heads(FAKE, D)), dict(dk=_heads(6 * FAKE, D)), dict(dv=_heads(7 * FAKE, D)),
-                dict(dq=_heads(5 * FAKE + 256))):
+                dict(dq=_heads(5 * FAKE + 256)), dict(dq=_heads()), dict(dq=_heads(5 * FAKE))):
         assert bwd(**bad) == INV, bad
-    assert bwd(dq=_heads()) == WS and bwd(dq=_heads(5 * FAKE)) == WS
     assert bwd(k=_heads(1 << 44, (1 << 22) + 8)) == UNS
     assert bwd(q=_heads(1 << 44, 1 << 23)) == UNS
     assert bwd(dout=_heads(1 << 44, D, 1 << 28)) == UNS
