@@ -11,7 +11,7 @@
 
 #include <algorithm>
 #include <functional>
-#include <queue>
+#include <utility>
 #include <vector>
 
 #include "../../include/upipe.h"
@@ -29,21 +29,27 @@ constexpr int64_t kMaxTokens = int64_t(1) << 40;
 // Elements from one token's row to the next: a stage of 128 rows is addressed with
 // 32-bit byte offsets.
 constexpr int64_t kMaxRowStride = int64_t(1) << 22;
-constexpr int64_t kMaxGrid = int64_t(1) << 30;
+// A launch counts its threads in 32 bits.
+bool grid_fits(int64_t blocks, int threads) { return blocks < (int64_t(1) << 32) / threads; }
 constexpr int kCUs = 256;
 
-// Time at which the last of these workgroups ends: each goes to the first of the CUs
-// that is free, in order, one to a CU.
-double makespan(const std::vector<float>& cost, int copies) {
-  std::priority_queue<double, std::vector<double>, std::greater<double>> free;
-  for (int i = 0; i < kCUs; ++i) free.push(0.0);
-  double end = 0.0;
-  for (float c : cost)
+// Time at which the last of these workgroups ends, `copies` of each: longest first,
+// each to the first of the CUs that is free, one to a CU, taking fixed + units * unit.
+double makespan(std::vector<int>* units, int copies, double fixed, double unit) {
+  std::sort(units->begin(), units->end(), std::greater<int>());
+  float free[kCUs] = {};           // a heap, the first free one on top
+  float end = 0.f;
+  for (int u : *units)
     for (int i = 0; i < copies; ++i) {
-      const double t = free.top() + c;
-      free.pop();
-      free.push(t);
+      const float t = free[0] + (float)(fixed + u * unit);
       end = std::max(end, t);
+      int at = 0;
+      for (int c; (c = 2 * at + 1) < kCUs; at = c) {
+        if (c + 1 < kCUs && free[c + 1] < free[c]) ++c;
+        if (free[c] >= t) break;
+        free[at] = free[c];
+      }
+      free[at] = t;
     }
   return end;
 }
@@ -82,35 +88,19 @@ int seq_parts(const Lengths& s, int most) {
   return std::max(1, std::min(kMostParts, (stages + most - 1) / most));
 }
 
-struct FwdWork {
-  RowItem item;
-  int stages, seq;
-};
-
-void fwd_work(const std::vector<Lengths>& seqs, int G, int causal, const FwdChoice& c,
-              std::vector<FwdWork>* out) {
+// Calls f(sequence, tile, part, parts, stages) for every workgroup of the forward.
+template <class F>
+void each_fwd(const std::vector<Lengths>& seqs, int G, int causal, const FwdChoice& c, F&& f) {
   const int rows = 256 / c.ks;
-  out->clear();
   for (size_t i = 0; i < seqs.size(); ++i) {
     const Lengths& s = seqs[i];
-    const int np = seq_parts(s, c.most), n = row_tiles(s.Lq, G, rows);
-    for (int t = n - 1; t >= 0; --t) {
+    const int np = seq_parts(s, c.most);
+    for (int t = row_tiles(s.Lq, G, rows) - 1; t >= 0; --t) {
       const int st = tile_stages(s, G, rows, t, causal), per = (st + np - 1) / np;
-      for (int p = 0; p < np; ++p) {
-        RowItem it{};
-        it.q0 = s.q0;
-        it.k0 = s.k0;
-        it.Lq = s.Lq;
-        it.Lk = s.Lk;
-        it.tile = t;
-        it.part = p;
-        it.parts = np;
-        out->push_back({it, std::max(0, std::min(st, per * (p + 1)) - per * p), (int)i});
-      }
+      for (int p = 0; p < np; ++p)
+        f((int)i, t, p, np, std::max(0, std::min(st, per * (p + 1)) - per * p));
     }
   }
-  std::stable_sort(out->begin(), out->end(),
-                   [](const FwdWork& a, const FwdWork& b) { return a.stages > b.stages; });
 }
 
 // The split of waves (1, 2 or 4 parts of a stage's keys) and of keys over
@@ -118,22 +108,18 @@ void fwd_work(const std::vector<Lengths>& seqs, int G, int causal, const FwdChoi
 // workgroups a CU on the largest tiles are the fastest.
 FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
   FwdChoice best;
-  int64_t tiles = 0;
-  for (const Lengths& s : seqs) tiles += row_tiles(s.Lq, G, 256);
-  if (tiles * Hkv >= 16 * kCUs) return best;
-  std::vector<FwdWork> work;
-  std::vector<float> cost;
+  std::vector<int> units;
   bool first = true;
+  // Stages of all workgroups.
   auto look = [&](FwdChoice c, int i) {
-    fwd_work(seqs, G, causal, c, &work);
-    cost.clear();
+    units.clear();
     int64_t parts = 0, stages = 0;
-    for (const FwdWork& w : work) {
-      cost.push_back((float)(kFwdFixed + w.stages * kFwdStage[i]));
-      parts += w.item.parts > 1;
-      stages += w.stages;
-    }
-    c.est = makespan(cost, Hkv);
+    each_fwd(seqs, G, causal, c, [&](int, int, int, int np, int st) {
+      units.push_back(st);
+      parts += np > 1;
+      stages += st;
+    });
+    c.est = makespan(&units, Hkv, kFwdFixed, kFwdStage[i]);
     if (parts > 0) c.est += kMergeFixed + kMergePart * parts * Hkv * (4.0 / c.ks);
     // parts take workspace: only for a gain
     if (first || c.est < (parts > 0 ? 0.95 : 1.0) * best.est) best = c;
@@ -143,7 +129,10 @@ FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causa
   for (int i = 0; i < 3; ++i) {
     FwdChoice c;
     c.ks = kFwdParts[i];
-    const int64_t mean = (look(c, i) + kCUs - 1) / kCUs;      // stages of a CU
+    const int64_t stages = look(c, i), mean = (stages + kCUs - 1) / kCUs;      // of a CU
+    // Near the whole chip's rate of the largest tiles: nothing to gain.
+    if (i == 0 && best.est <= 1.1 * stages * kFwdStage[0] / kCUs) break;
+    if (units.empty() || units[0] <= 2 * mean) continue;       // no long ones to cut
     for (int64_t m : {mean, 2 * mean}) {
       c.most = (int)std::max<int64_t>(4, m);
       look(c, i);
@@ -164,82 +153,57 @@ void key_walk(const Lengths& s, int tpt, int kb, int causal, int* first, int* la
   *first = (int)std::min<int64_t>(tok / tpt, *last + 1);
 }
 
-// The walks of a sequence's key blocks are prefixes of one list, its tiles from the
-// last one down.  That list is cut at every `most`-th tile, so that the workgroups of
-// a segment walk the same tiles side by side and share their lines in L2 (walks cut
-// each into even segments: 32768 rows of 8 heads on 1, 4330 us).
-void key_work(const std::vector<Lengths>& seqs, int G, int causal, int most,
-              std::vector<KeyItem>* keys, std::vector<FoldItem>* folds, int64_t* slots) {
+// Calls f(sequence, r0, key block, segment, segments, first tile, tiles) for every
+// workgroup of dK/dV.  The walks of a sequence's key blocks are prefixes of one list,
+// its tiles from the last one down.  That list is cut at every `most`-th tile, so that
+// the workgroups of a segment walk the same tiles side by side and share their lines
+// in L2 (walks cut each into even segments: 32768 rows of 8 heads on 1, 4330 | 4207 us).
+template <class F>
+void each_key(const std::vector<Lengths>& seqs, int G, int causal, int most, F&& f) {
   const int tpt = tile_tokens(G);
-  keys->clear();
-  folds->clear();
-  *slots = 0;
   int64_t r0 = 0;
-  for (const Lengths& s : seqs) {
-    const int nkb = (s.Lk + 127) / 128;
-    for (int kb = 0; kb < nkb; ++kb) {
+  for (size_t s = 0; s < seqs.size(); ++s) {
+    for (int kb = 0; kb < (seqs[s].Lk + 127) / 128; ++kb) {
       int first, last;
-      key_walk(s, tpt, kb, causal, &first, &last);
+      key_walk(seqs[s], tpt, kb, causal, &first, &last);
       const int n = last - first + 1, segs = n <= most ? 1 : (n + most - 1) / most;
-      KeyItem it{};
-      it.q0 = s.q0;
-      it.k0 = s.k0;
-      it.r0 = r0;
-      it.Lq = s.Lq;
-      it.Lk = s.Lk;
-      it.kb = kb;
-      for (int i = 0; i < segs; ++i) {
-        it.first = last - i * most * (segs > 1);
-        it.count = std::min(n - i * most * (segs > 1), most);
-        it.slot = segs > 1 ? (int32_t)(*slots + i) : -1;
-        keys->push_back(it);
-      }
-      if (segs > 1) {
-        folds->push_back({s.k0, s.Lk, kb, (int32_t)*slots, segs});
-        *slots += segs;
-      }
+      for (int i = 0, done = 0; i < segs; ++i, done += most)
+        f((int)s, r0, kb, i, segs, last - done, segs > 1 ? std::min(n - done, most) : n);
     }
-    r0 += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
+    r0 += (int64_t)((seqs[s].Lq + tpt - 1) / tpt) * 128;
   }
-  std::stable_sort(keys->begin(), keys->end(), [](const KeyItem& a, const KeyItem& b) {
-    if (a.count != b.count) return a.count > b.count;
-    if (a.k0 != b.k0) return a.k0 < b.k0;
-    return a.first > b.first;
-  });
 }
 
 // The longest segment with which all of them are expected to end first: the longest
-// walk in n / 8 parts.  Many key blocks need no look.
+// walk in n / 8 parts.
 int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
   const int tpt = tile_tokens(G), whole = 1 << 30;
-  int64_t blocks = 0;
   int longest = 1;
-  for (const Lengths& s : seqs) {
-    blocks += (s.Lk + 127) / 128;
+  for (const Lengths& s : seqs)
     if (s.Lk > 0) longest = std::max(longest, (s.Lq + tpt - 1) / tpt);
-  }
-  if (blocks * Hkv > 32 * kCUs) return whole;
-  std::vector<KeyItem> keys;
-  std::vector<FoldItem> folds;
-  std::vector<float> cost;
-  int64_t slots;
+  std::vector<int> units;
   int best = whole, tried = 0;
   double best_est = 0.0;
   for (int n : {8, 10, 12, 14, 16, 18, 20, 24, 28, 32, 36, 40, 48, 56, 64, 80, 96, 128}) {
     const int most = (int)(((int64_t)longest * 8 + n - 1) / n);
     if (most == tried) continue;
     tried = most;
-    key_work(seqs, G, causal, most, &keys, &folds, &slots);
+    int64_t slots = 0, tiles = 0;
+    units.clear();
+    each_key(seqs, G, causal, most, [&](int, int64_t, int, int, int segs, int, int count) {
+      units.push_back(count);
+      slots += segs > 1;
+      tiles += count;
+    });
     if (n > 8 && slots * Hkv > kMaxSums) continue;
-    cost.clear();
-    for (const KeyItem& k : keys) cost.push_back((float)(kKeyFixed + k.count * kKeyTile));
-    const double est =
-        makespan(cost, Hkv) + (slots > 0 ? kFoldFixed + kFoldSum * slots * Hkv : 0.0);
+    const double est = makespan(&units, Hkv, kKeyFixed, kKeyTile) +
+                       (slots > 0 ? kFoldFixed + kFoldSum * slots * Hkv : 0.0);
     if (n == 8 || est < best_est) {
       best = most;
       best_est = est;
     }
-    if (most <= 2) break;
+    // Near the whole chip's rate, or segments of next to nothing.
+    if (best_est <= 1.03 * tiles * Hkv * kKeyTile / kCUs || most <= 2) break;
   }
   return best;
 }
@@ -247,44 +211,45 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
 // us of a dQ stage with 1 (64 keys), 2 and 4 (128 keys) key parts on a full chip.
 constexpr double kDqStage[3] = {2.5, 2.8, 1.6}, kDqFixed = 4.0;
 
-struct DqWork {
-  TileItem item;
-  int stages;
-};
-
-void dq_work(const std::vector<Lengths>& seqs, int G, int causal, int ks, std::vector<DqWork>* out) {
+// Calls f(sequence, r0, tile, stages) for every workgroup of dQ.
+template <class F>
+void each_dq(const std::vector<Lengths>& seqs, int G, int causal, int ks, F&& f) {
   const int rows = 256 / ks, tpt = tile_tokens(G);
-  out->clear();
   int64_t r0 = 0;
-  for (const Lengths& s : seqs) {
-    for (int t = row_tiles(s.Lq, G, rows) - 1; t >= 0; --t)
-      out->push_back({{s.q0, s.k0, r0, s.Lq, s.Lk, t, 0},
-                      tile_stages(s, G, rows, t, causal) * (ks == 1 ? 2 : 1)});
-    r0 += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
+  for (size_t s = 0; s < seqs.size(); ++s) {
+    for (int t = row_tiles(seqs[s].Lq, G, rows) - 1; t >= 0; --t)
+      f((int)s, r0, t, tile_stages(seqs[s], G, rows, t, causal) * (ks == 1 ? 2 : 1));
+    r0 += (int64_t)((seqs[s].Lq + tpt - 1) / tpt) * 128;
   }
-  std::stable_sort(out->begin(), out->end(),
-                   [](const DqWork& a, const DqWork& b) { return a.stages > b.stages; });
 }
 
 int choose_dq(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
-  int64_t tiles = 0;
-  for (const Lengths& s : seqs) tiles += row_tiles(s.Lq, G, 256);
-  if (tiles * Hkv >= 16 * kCUs) return 1;
-  std::vector<DqWork> work;
-  std::vector<float> cost;
+  std::vector<int> units;
   int best = 1;
   double best_est = 0.0;
   for (int i = 0; i < 3; ++i) {
-    dq_work(seqs, G, causal, kFwdParts[i], &work);
-    cost.clear();
-    for (const DqWork& w : work) cost.push_back((float)(kDqFixed + w.stages * kDqStage[i]));
-    const double est = makespan(cost, Hkv);
+    int64_t stages = 0;
+    units.clear();
+    each_dq(seqs, G, causal, kFwdParts[i], [&](int, int64_t, int, int st) {
+      units.push_back(st);
+      stages += st;
+    });
+    const double est = makespan(&units, Hkv, kDqFixed, kDqStage[i]);
     if (i == 0 || est < best_est) {
       best = kFwdParts[i];
       best_est = est;
     }
+    if (i == 0 && est <= 1.1 * stages * Hkv * kDqStage[0] / kCUs) break;
   }
   return best;
+}
+
+// Longest first, in the order they came.
+template <class T>
+void longest_first(std::vector<std::pair<int, T>>* work, std::vector<T>* out) {
+  std::stable_sort(work->begin(), work->end(),
+                   [](const auto& a, const auto& b) { return a.first > b.first; });
+  for (const auto& w : *work) out->push_back(w.second);
 }
 
 int check_lengths(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, int d, int causal,
@@ -341,8 +306,6 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   }
 
   const FwdChoice c = choose_fwd(seqs, G, Hkv, causal);
-  std::vector<FwdWork> work;
-  fwd_work(seqs, G, causal, c, &work);
   h.fwd_ks = c.ks;
   // Partial rows: [parts][Lq][Hq] of every sequence that is cut.
   std::vector<int64_t> p0;
@@ -359,10 +322,12 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
       p->merge.push_back({s.q0, h.part_rows, s.Lq, np, (int32_t)b, 0});
     h.part_rows += np * rows;
   }
-  for (FwdWork& w : work) {
-    w.item.p0 = p0[w.seq];
-    p->fwd.push_back(w.item);
-  }
+  std::vector<std::pair<int, RowItem>> fwd;
+  each_fwd(seqs, G, causal, c, [&](int i, int tile, int part, int np, int stages) {
+    const Lengths& s = seqs[i];
+    fwd.push_back({stages, {s.q0, s.k0, p0[i], s.Lq, s.Lk, tile, part, np, 0}});
+  });
+  longest_first(&fwd, &p->fwd);
 
   const int tpt = tile_tokens(G);
   for (const Lengths& s : seqs) {
@@ -370,15 +335,30 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
       p->terms.push_back({s.q0, s.k0, h.term_rows, s.Lq, s.Lk, t, 0});
     h.term_rows += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
   }
-  key_work(seqs, G, causal, choose_segment(seqs, G, Hkv, causal), &p->keys, &p->folds, &h.slots);
+  std::vector<std::pair<int, KeyItem>> keys;
+  each_key(seqs, G, causal, choose_segment(seqs, G, Hkv, causal),
+           [&](int i, int64_t r0, int kb, int seg, int segs, int first, int count) {
+             const Lengths& s = seqs[i];
+             if (seg == 0 && segs > 1) p->folds.push_back({s.k0, s.Lk, kb, (int32_t)h.slots, segs});
+             const int32_t slot = segs > 1 ? (int32_t)h.slots++ : -1;
+             keys.push_back({count, {s.q0, s.k0, r0, s.Lq, s.Lk, kb, first, count, slot}});
+           });
+  // of one length, the workgroups of a segment side by side
+  std::stable_sort(keys.begin(), keys.end(), [](const auto& a, const auto& b) {
+    return a.second.r0 != b.second.r0 ? a.second.r0 < b.second.r0 : a.second.first > b.second.first;
+  });
+  longest_first(&keys, &p->keys);
   h.dq_ks = choose_dq(seqs, G, Hkv, causal);
-  std::vector<DqWork> dqs;
-  dq_work(seqs, G, causal, h.dq_ks, &dqs);
-  for (const DqWork& w : dqs) p->dqs.push_back(w.item);
+  std::vector<std::pair<int, TileItem>> dqs;
+  each_dq(seqs, G, causal, h.dq_ks, [&](int i, int64_t r0, int tile, int stages) {
+    const Lengths& s = seqs[i];
+    dqs.push_back({stages, {s.q0, s.k0, r0, s.Lq, s.Lk, tile, 0}});
+  });
+  longest_first(&dqs, &p->dqs);
 
-  for (size_t n : {p->terms.size() * 4, p->keys.size(), p->dqs.size(), p->folds.size() * 16})
-    if ((int64_t)n * Hkv > kMaxGrid) return UPIPE_ERR_UNSUPPORTED;
-  if ((int64_t)p->fwd.size() * Hkv > kMaxGrid || (int64_t)p->merge.size() > kMaxGrid)
+  auto fits = [&](size_t items, int threads) { return grid_fits((int64_t)items * Hkv, threads); };
+  if (!fits(p->fwd.size(), 512) || !fits(p->merge.size(), 256) || !fits(p->terms.size() * 4, 256) ||
+      !fits(p->keys.size(), 256) || !fits(p->folds.size() * 16, 256) || !fits(p->dqs.size(), 512))
     return UPIPE_ERR_UNSUPPORTED;
   h.n_fwd = (int32_t)p->fwd.size();
   h.n_merge = (int32_t)p->merge.size();
@@ -494,7 +474,8 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
         (Tk > 0 && (!heads_ok(k, Tk, Hkv) || !heads_ok(v, Tk, Hkv))))
       return UPIPE_ERR_INVALID_ARG;
     // o may be q: a workgroup reads its rows before it writes them.
-    if ((!heads_same(o, q) && !apart(o, Tq, Hq, q, Tq, Hq)) || !apart(o, Tq, Hq, k, Tk, Hkv) ||
+    if ((!heads_same(o, q) && !apart(o, Tq, Hq, q, Tq, Hq)) ||
+        !apart(o, Tq, Hq, k, Tk, Hkv) ||
         !apart(o, Tq, Hq, v, Tk, Hkv))
       return UPIPE_ERR_INVALID_ARG;
     if (!stage_rows(k) || !stage_rows(v)) return UPIPE_ERR_UNSUPPORTED;
@@ -625,7 +606,8 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
     return UPIPE_ERR_INVALID_ARG;
   if (d != HEAD_DIM || Hq > kMaxHeads || cap > kMaxSeq || P > kMaxSeq || nq > 128 || B > 65536)
     return UPIPE_ERR_UNSUPPORTED;
-  return UPIPE_OK;
+  // a row's sixteen lanes, or workgroups of 64 packed rows, a few parts each
+  return grid_fits(B * nq * Hq, 512) ? UPIPE_OK : UPIPE_ERR_UNSUPPORTED;
 }
 
 // The lengths are on the device: the cut goes by the capacity, and a part is the
@@ -649,8 +631,8 @@ CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv)
 }
 
 // The rows of o outside the range of all caches.
-bool apart_cache(const upipe_heads& o, int64_t T, int Hq, const upipe_heads& k, int64_t batch, int64_t B,
-                 int64_t cap, int Hkv) {
+bool apart_cache(const upipe_heads& o, int64_t T, int Hq, const upipe_heads& k, int64_t batch,
+                 int64_t B, int64_t cap, int Hkv) {
   const int64_t so = (T - 1) * o.row + (Hq - 1) * o.head + HEAD_DIM;
   const int64_t sk = (B - 1) * batch + (cap - 1) * k.row + (Hkv - 1) * k.head + HEAD_DIM;
   return !overlap(o.p, 2 * so, k.p, 2 * sk);
@@ -680,13 +662,14 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     if (rc != UPIPE_OK) return rc;
     const int64_t T = B * nq, most = int64_t(1) << 60;
     if (!heads_ok(q, T, Hq) || !heads_ok(o, T, Hq) || !heads_distinct(o, T, Hq) ||
-        !heads_ok(k, cap, Hkv) || !heads_ok(v, cap, Hkv) || !lens || ((uintptr_t)lens & 3) != 0 || !aligned16(lse) ||
-        !aligned16(ws) || k_cache < 0 || v_cache < 0 || k_cache % 8 != 0 || v_cache % 8 != 0 ||
-        k_cache > most / B || v_cache > most / B)
+        !heads_ok(k, cap, Hkv) || !heads_ok(v, cap, Hkv) || !lens || ((uintptr_t)lens & 3) != 0 ||
+        !aligned16(lse) || !aligned16(ws) || k_cache < 0 || v_cache < 0 || k_cache % 8 != 0 ||
+        v_cache % 8 != 0 || k_cache > most / B || v_cache > most / B)
       return UPIPE_ERR_INVALID_ARG;
     if (P > 0 && (!heads_ok(k_prefix, P, Hkv) || !heads_ok(v_prefix, P, Hkv)))
       return UPIPE_ERR_INVALID_ARG;
-    if ((!heads_same(o, q) && !apart(o, T, Hq, q, T, Hq)) || !apart_cache(o, T, Hq, k, k_cache, B, cap, Hkv) ||
+    if ((!heads_same(o, q) && !apart(o, T, Hq, q, T, Hq)) ||
+        !apart_cache(o, T, Hq, k, k_cache, B, cap, Hkv) ||
         !apart_cache(o, T, Hq, v, v_cache, B, cap, Hkv) ||
         (P > 0 && (!apart(o, T, Hq, k_prefix, P, Hkv) || !apart(o, T, Hq, v_prefix, P, Hkv))))
       return UPIPE_ERR_INVALID_ARG;

@@ -185,7 +185,8 @@ def test_refusals():
                 dict(o=_heads(5 * FAKE))):
         assert _call(**bad) == INV, bad
     for bad in (dict(d=64), dict(Hq=65), dict(nq=129), dict(cap=1 << 24), dict(P=1 << 24),
-                dict(B=65537), dict(k=_heads(2 * FAKE, (1 << 22) + 8))):
+                dict(B=65537), dict(B=65536, nq=128, Hq=64, Hkv=1, k_cache=0, v_cache=0),
+                dict(k=_heads(2 * FAKE, (1 << 22) + 8))):
         assert _call(**bad) == UNS, bad
     assert _call(o=_heads()) == WS           # over its own queries
     assert _call(P=0, kp=_heads(0), vp=_heads(0)) == WS
