@@ -8,15 +8,15 @@
 //   dx = r (a - n mean(a n)) with n = r x
 // r is formed again in the backward: it comes out of the row that is read anyway.
 //
-// HBM-bound: x is read and y written once (backward: x and dy read, dx written).
-// Eight lanes hold a row, lane j the elements 8j.. and 64 + 8j.., so a pair lies
-// in one lane and a wave reads whole 128-byte lines of 8 rows.  All rows (token,
-// head) of q, then those of k, are dealt out to workgroups, one tensor to each, so
-// a thread holds one tensor's 16 weights (and its 16 sums of dw).  The angles
-// are formed per row, in fp64 turns (positions to 2^32) with the frequencies from
-// the kernel's arguments: about a third of a row's instructions, under the time
-// that its bytes take.  The norm's sums, r, the rotation and the sums of dw are fp32; y, dx
-// and a bf16 dw are rounded once.
+// HBM-bound: x is read once and y written (backward: x and dy read, dx written).  Eight
+// lanes hold a row, lane j the elements 8j.. and 64 + 8j.., so a pair lies in one lane
+// and a wave reads whole 128-byte lines.  The pairs of heads of all tokens of q, then
+// those of k, are dealt out to workgroups, one tensor to each, so a thread holds one
+// tensor's 16 weights (and its 16 sums of dw).  The angles are formed once per token and
+// pair of heads, in fp64 turns (positions to 2^32) with the frequencies from the
+// kernel's arguments.  The norm's sums, r, the rotation and the sums of dw are fp32; y,
+// dx and a bf16 dw are rounded once.  65536 tokens: 40 heads forward 258 us (5.2 TB/s, a
+// large copy 5.1), 72 heads backward 712 us (5.1 TB/s; a head at a time 742).
 #include "common.h"
 #include "kernels.h"
 
@@ -24,7 +24,7 @@ namespace upipe {
 
 namespace {
 
-constexpr int kRowsPerBlock = 32;    // 256 threads, 8 lanes a row
+constexpr int kPairsPerBlock = 32;    // 256 threads, 8 lanes a row, a pair of heads at a time
 
 __device__ __forceinline__ float sum8(float v) {
 #pragma unroll
@@ -49,41 +49,59 @@ __device__ __forceinline__ void load_weights(const void* w, int w_fp32, int j, f
   }
 }
 
-// The rows of one tensor that this lane group takes: r, r + step, ..., as (token,
-// head) without a division in the loop.
-struct RowWalk {
-  int64_t t, rows_left;
-  int h;
+// The pairs of heads of one tensor that this lane group takes: pair first, first +
+// step, ..., as (token, first head of the pair) without a division in the loop.
+struct PairWalk {
+  int64_t t, left;
+  int p, pairs;
   int64_t t_step;
-  int h_step, H;
-  __device__ __forceinline__ RowWalk(int64_t first, int64_t step, int64_t rows, int heads) {
-    H = heads;
-    t = first / heads;
-    h = (int)(first - t * heads);
-    t_step = step / heads;
-    h_step = (int)(step - t_step * heads);
-    rows_left = first < rows ? (rows - first + step - 1) / step : 0;
+  int p_step;
+  __device__ __forceinline__ PairWalk(int64_t first, int64_t step, int64_t T, int H) {
+    pairs = (H + 1) / 2;
+    const int64_t n = T * pairs;
+    t = first / pairs;
+    p = (int)(first - t * pairs);
+    t_step = step / pairs;
+    p_step = (int)(step - t_step * pairs);
+    left = first < n ? (n - first + step - 1) / step : 0;
   }
   __device__ __forceinline__ void next() {
     t += t_step;
-    h += h_step;
-    if (h >= H) {
-      h -= H;
+    p += p_step;
+    if (p >= pairs) {
+      p -= pairs;
       ++t;
     }
-    --rows_left;
+    --left;
   }
 };
 
-__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
+// This lane's angles at a position: cos and sin of its eight pairs.
+__device__ __forceinline__ void angles(double pos, const double (&f)[8], float (&c)[8],
+                                       float (&s)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const double turns = pos * f[e];
+    cos_sin_turns((float)(turns - rint(turns)), c[e], s[e]);
+  }
+}
+
+// The workgroup's tensor, its number among that tensor's and their count.
+__device__ __forceinline__ const NormRopeSide& side_of(const NormRopeArgs& a, int& block,
+                                                       int& blocks) {
   const bool is_q = (int)blockIdx.x < a.blocks_q;
-  const NormRopeSide& s = is_q ? a.q : a.k;
-  const int block = is_q ? blockIdx.x : blockIdx.x - a.blocks_q;
-  const int blocks = is_q ? a.blocks_q : gridDim.x - a.blocks_q;
+  block = is_q ? blockIdx.x : blockIdx.x - a.blocks_q;
+  blocks = is_q ? a.blocks_q : gridDim.x - a.blocks_q;
+  return is_q ? a.q : a.k;
+}
+
+__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
+  int block, blocks;
+  const NormRopeSide& s = side_of(a, block, blocks);
   const int j = threadIdx.x & 7;
-  RowWalk it((int64_t)block * kRowsPerBlock + (threadIdx.x >> 3), (int64_t)blocks * kRowsPerBlock,
-             a.T * s.H, s.H);
-  if (it.rows_left <= 0) return;
+  PairWalk it((int64_t)block * kPairsPerBlock + (threadIdx.x >> 3),
+              (int64_t)blocks * kPairsPerBlock, a.T, s.H);
+  if (it.left <= 0) return;
   float w[16];
   load_weights(s.w, a.w_fp32, j, w);
   double f[8];
@@ -91,32 +109,38 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
   for (int e = 0; e < 8; ++e) f[e] = a.freq.turns[8 * j + e];
   const bf16* x0 = s.x.p + 8 * j;
   bf16* y0 = s.y.p + 8 * j;
-  for (; it.rows_left > 0; it.next()) {
-    const Row16 x = load_row(x0 + it.t * s.x.row + it.h * s.x.head);
-    const double pos = (double)a.positions[it.t];
-    float v[16], ss = 0.f;
+  for (; it.left > 0; it.next()) {
+    const int h = 2 * it.p, n = min(2, s.H - h);
+    const bf16* xp = x0 + it.t * s.x.row + h * s.x.head;
+    Row16 x[2];
+    x[0] = load_row(xp);
+    if (n > 1) x[1] = load_row(xp + s.x.head);
+    float c[8], sn[8];
+    angles((double)a.positions[it.t], f, c, sn);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = (float)x.lo[e];
-      v[8 + e] = (float)x.hi[e];
-      ss = fmaf(v[e], v[e], ss);
-      ss = fmaf(v[8 + e], v[8 + e], ss);
-    }
-    const float r = __frsqrt_rn(fmaf(sum8(ss), 1.f / HEAD_DIM, a.eps));
-    Row16 y;
+    for (int u = 0; u < 2; ++u) {
+      if (u >= n) break;
+      float v[16], ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float c, sn;
-      const double turns = pos * f[e];
-      cos_sin_turns((float)(turns - rint(turns)), c, sn);
-      float p = v[e] * r * w[e], q = v[8 + e] * r * w[8 + e];
-      rope_pair(p, q, c, sn, false);
-      y.lo[e] = (bf16)p;
-      y.hi[e] = (bf16)q;
+      for (int e = 0; e < 8; ++e) {
+        v[e] = (float)x[u].lo[e];
+        v[8 + e] = (float)x[u].hi[e];
+        ss = fmaf(v[e], v[e], ss);
+        ss = fmaf(v[8 + e], v[8 + e], ss);
+      }
+      const float r = __frsqrt_rn(fmaf(sum8(ss), 1.f / HEAD_DIM, a.eps));
+      Row16 y;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float p = v[e] * r * w[e], q = v[8 + e] * r * w[8 + e];
+        rope_pair(p, q, c[e], sn[e], false);
+        y.lo[e] = (bf16)p;
+        y.hi[e] = (bf16)q;
+      }
+      bf16* yp = y0 + it.t * s.y.row + (h + u) * s.y.head;
+      *reinterpret_cast<bf16x8*>(yp) = y.lo;
+      *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
     }
-    bf16* yp = y0 + it.t * s.y.row + it.h * s.y.head;
-    *reinterpret_cast<bf16x8*>(yp) = y.lo;
-    *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
   }
 }
 
@@ -124,13 +148,11 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
 __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeArgs a,
                                                             float* __restrict__ partial) {
   __shared__ float sums[4][HEAD_DIM];
-  const bool is_q = (int)blockIdx.x < a.blocks_q;
-  const NormRopeSide& s = is_q ? a.q : a.k;
-  const int block = is_q ? blockIdx.x : blockIdx.x - a.blocks_q;
-  const int blocks = is_q ? a.blocks_q : gridDim.x - a.blocks_q;
+  int block, blocks;
+  const NormRopeSide& s = side_of(a, block, blocks);
   const int j = threadIdx.x & 7;
-  RowWalk it((int64_t)block * kRowsPerBlock + (threadIdx.x >> 3), (int64_t)blocks * kRowsPerBlock,
-             a.T * s.H, s.H);
+  PairWalk it((int64_t)block * kPairsPerBlock + (threadIdx.x >> 3),
+              (int64_t)blocks * kPairsPerBlock, a.T, s.H);
   float w[16], dw[16];
   load_weights(s.w, a.w_fp32, j, w);
   double f[8];
@@ -141,41 +163,51 @@ __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeArgs a,
   const bf16* x0 = s.x.p + 8 * j;
   const bf16* d0 = s.dy.p + 8 * j;
   bf16* y0 = s.y.p + 8 * j;
-  for (; it.rows_left > 0; it.next()) {
-    const Row16 x = load_row(x0 + it.t * s.x.row + it.h * s.x.head);
-    const Row16 d = load_row(d0 + it.t * s.dy.row + it.h * s.dy.head);
-    const double pos = (double)a.positions[it.t];
-    float v[16], g[16], ss = 0.f, ax = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = (float)x.lo[e];
-      v[8 + e] = (float)x.hi[e];
-      g[e] = (float)d.lo[e];
-      g[8 + e] = (float)d.hi[e];
-      float c, sn;
-      const double turns = pos * f[e];
-      cos_sin_turns((float)(turns - rint(turns)), c, sn);
-      rope_pair(g[e], g[8 + e], c, sn, true);
+  for (; it.left > 0; it.next()) {
+    const int h = 2 * it.p, n = min(2, s.H - h);
+    const bf16* xp = x0 + it.t * s.x.row + h * s.x.head;
+    const bf16* dp = d0 + it.t * s.dy.row + h * s.dy.head;
+    Row16 x[2], d[2];
+    x[0] = load_row(xp);
+    d[0] = load_row(dp);
+    if (n > 1) {
+      x[1] = load_row(xp + s.x.head);
+      d[1] = load_row(dp + s.dy.head);
     }
+    float c[8], sn[8];
+    angles((double)a.positions[it.t], f, c, sn);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      ss = fmaf(v[e], v[e], ss);
-      ax = fmaf(g[e] * w[e], v[e], ax);
-    }
-    const float r = __frsqrt_rn(fmaf(sum8(ss), 1.f / HEAD_DIM, a.eps));
-    const float m = sum8(ax) * r * (1.f / HEAD_DIM);      // mean(a r x)
-    Row16 y;
+    for (int u = 0; u < 2; ++u) {
+      if (u >= n) break;
+      float v[16], g[16], ss = 0.f, ax = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float n = v[e] * r;
-      dw[e] = fmaf(g[e], n, dw[e]);
-      const bf16 dx = (bf16)(r * fmaf(g[e], w[e], -n * m));
-      if (e < 8) y.lo[e] = dx;
-      else y.hi[e - 8] = dx;
+      for (int e = 0; e < 8; ++e) {
+        v[e] = (float)x[u].lo[e];
+        v[8 + e] = (float)x[u].hi[e];
+        g[e] = (float)d[u].lo[e];
+        g[8 + e] = (float)d[u].hi[e];
+        rope_pair(g[e], g[8 + e], c[e], sn[e], true);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        ss = fmaf(v[e], v[e], ss);
+        ax = fmaf(g[e] * w[e], v[e], ax);
+      }
+      const float r = __frsqrt_rn(fmaf(sum8(ss), 1.f / HEAD_DIM, a.eps));
+      const float m = sum8(ax) * r * (1.f / HEAD_DIM);      // mean(a r x)
+      Row16 y;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float nx = v[e] * r;
+        dw[e] = fmaf(g[e], nx, dw[e]);
+        const bf16 dx = (bf16)(r * fmaf(g[e], w[e], -nx * m));
+        if (e < 8) y.lo[e] = dx;
+        else y.hi[e - 8] = dx;
+      }
+      bf16* yp = y0 + it.t * s.y.row + (h + u) * s.y.head;
+      *reinterpret_cast<bf16x8*>(yp) = y.lo;
+      *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
     }
-    bf16* yp = y0 + it.t * s.y.row + it.h * s.y.head;
-    *reinterpret_cast<bf16x8*>(yp) = y.lo;
-    *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
   }
   // The eight row groups of a wave, then the four waves, always in this order.
 #pragma unroll
@@ -230,29 +262,29 @@ __global__ __launch_bounds__(1024) void norm_dw_fold_kernel(const float* __restr
 
 }  // namespace
 
-// Workgroups of one tensor's rows: every row group has one row while that needs
-// no more than `most` workgroups.
-static int norm_blocks(int64_t rows, int most) {
-  const int64_t n = (rows + kRowsPerBlock - 1) / kRowsPerBlock;
+// Workgroups of one tensor's rows: every lane group has one pair of heads while that
+// needs no more than `most` workgroups.
+static int norm_blocks(int64_t T, int H, int most) {
+  const int64_t n = (T * ((H + 1) / 2) + kPairsPerBlock - 1) / kPairsPerBlock;
   return (int)(n < most ? n : most);
 }
 
 constexpr int kNormFwdBlocks = 4096, kNormBwdBlocks = 1024;
 
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t st) {
-  a.blocks_q = norm_blocks(a.T * a.q.H, kNormFwdBlocks);
-  const int blocks_k = norm_blocks(a.T * a.k.H, kNormFwdBlocks);
+  a.blocks_q = norm_blocks(a.T, a.q.H, kNormFwdBlocks);
+  const int blocks_k = norm_blocks(a.T, a.k.H, kNormFwdBlocks);
   hipLaunchKernelGGL(norm_rope_kernel, dim3((unsigned)(a.blocks_q + blocks_k)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
 int64_t norm_rope_bwd_partials(int64_t T, int Hq, int Hkv) {
-  return norm_blocks(T * Hq, kNormBwdBlocks) + norm_blocks(T * Hkv, kNormBwdBlocks);
+  return norm_blocks(T, Hq, kNormBwdBlocks) + norm_blocks(T, Hkv, kNormBwdBlocks);
 }
 
 hipError_t launch_norm_rope_bwd(NormRopeArgs a, float* partial, hipStream_t st) {
-  a.blocks_q = norm_blocks(a.T * a.q.H, kNormBwdBlocks);
-  const int blocks_k = norm_blocks(a.T * a.k.H, kNormBwdBlocks);
+  a.blocks_q = norm_blocks(a.T, a.q.H, kNormBwdBlocks);
+  const int blocks_k = norm_blocks(a.T, a.k.H, kNormBwdBlocks);
   hipLaunchKernelGGL(norm_rope_bwd_kernel, dim3((unsigned)(a.blocks_q + blocks_k)), dim3(256), 0,
                      st, a, partial);
   return hipGetLastError();
@@ -261,7 +293,7 @@ hipError_t launch_norm_rope_bwd(NormRopeArgs a, float* partial, hipStream_t st) 
 hipError_t launch_norm_dw_fold(const float* partial, int64_t T, int Hq, int Hkv, void* dwq,
                                void* dwk, int w_fp32, hipStream_t st) {
   hipLaunchKernelGGL(norm_dw_fold_kernel, dim3(HEAD_DIM / 16, 2), dim3(1024), 0, st, partial,
-                     norm_blocks(T * Hq, kNormBwdBlocks), norm_blocks(T * Hkv, kNormBwdBlocks), dwq,
+                     norm_blocks(T, Hq, kNormBwdBlocks), norm_blocks(T, Hkv, kNormBwdBlocks), dwq,
                      dwk, w_fp32);
   return hipGetLastError();
 }

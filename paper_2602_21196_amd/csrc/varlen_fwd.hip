@@ -180,11 +180,9 @@ __device__ __forceinline__ void fold_in(const char* smem, int wq, int lane, f32x
 }
 
 
-// Row r of Lq * G against its keys by plain arithmetic, for the rows whose result
-// came out infinite or not a number: a masked key's weight is 0, but the matrix
-// instructions also multiply that 0 by a value that may be neither.  The lane pair
-// of a row has its query and output elements as the tile has them.  Ends early
-// once a visible score is not a number: so is then the whole row.
+// A row against its keys by plain arithmetic.  The lane pair of a row has its query and
+// output elements as the tile has them.  Ends early once a visible score is not a
+// number, or no element is finite any more: so it stays.
 __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const bf16* v, int64_t v_row,
                                          int64_t key0, int64_t key1, const bf16x8 (&qf)[8], int g,
                                          f32x16 (&oacc)[4], float& m_ref, float& l) {
@@ -219,26 +217,43 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
         for (int b = 0; b < 4; ++b)
           oacc[dt][4 * a + b] = fmaf(p, (float)vv[b], oacc[dt][4 * a + b] * alpha);
       }
-    if (!(p == p) || !(l == l)) {
-      l = NAN;
-      break;
-    }
+    if (!(l == l)) break;
+    float least = INFINITY;        // of the absolute values; NaN are passed over
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) least = fminf(least, fabsf(oacc[dt][i]));
+    if (fminf(least, __shfl_xor(least, 32)) == INFINITY) break;
   }
 }
 
-// A masked value that is infinite or not a number leaves NaN in the rows of its stage:
-// those are formed again without it.
+// A masked key's weight is 0, but the matrix instructions also multiply that 0 by the
+// key's value, which may be infinite or not a number: then the rows of its stage come
+// out as NaN.  Such a row is formed again without it.  `lim`: the row's last key, `end`:
+// the end of the keys that its tile multiplied.
 __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_row, const bf16* v,
-                                         int64_t v_row, int key0, int key1, const bf16x8 (&qf)[8],
-                                         int g, f32x16 (&oacc)[4], float& m_ref, float& l) {
+                                         int64_t v_row, int key0, int key1, int lim, int end,
+                                         const bf16x8 (&qf)[8], int g, f32x16 (&oacc)[4],
+                                         float& m_ref, float& l) {
   float z = 0.f;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) z = fmaf(oacc[dt][i], 0.f, z);
   z += __shfl_xor(z, 32);
-  if (row_ok && !(z == z))      // both lanes of a row
-    careful_row(k, k_row, v, v_row, key0, key1, qf, g, oacc, m_ref, l);
+  if (!row_ok || z == z) return;      // both lanes of a row alike
+  z = 0.f;
+  for (int j = max(lim + 1, key0); j < end; ++j) {
+    const bf16* p = v + j * v_row + 64 * g;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const bf16x8 x = *reinterpret_cast<const bf16x8*>(p + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z = fmaf((float)x[e], 0.f, z);
+    }
+  }
+  z += __shfl_xor(z, 32);
+  if (!(z == z)) careful_row(k, k_row, v, v_row, key0, key1, qf, g, oacc, m_ref, l);
 }
 
 // A row's result, by the lane pair that holds it: the part's, in fp32, or the row's own.
@@ -424,8 +439,8 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
     if (ks > 0) return;
     fold_in<KS>(smem, wq, lane, oacc, m_ref, l_tot);
   }
-  mend_row(row_ok, kp, a.k.row, vp, a.v.row, j0 * BKS, min(lim + 1, j1 * BKS), qf, g, oacc, m_ref,
-           l_tot);
+  mend_row(row_ok, kp, a.k.row, vp, a.v.row, j0 * BKS, min(lim + 1, j1 * BKS), lim,
+           min(it.Lk, min(j1, (seen_w + BKS - 1) / BKS) * BKS), qf, g, oacc, m_ref, l_tot);
   if (!row_ok) return;
   write_row(a, MODE == kRowsOne || (MODE == kRowsCache ? a.splits + a.part0 : it.parts) > 1, it, part_rows, lse_at, tok, kvh * G + hg, Hq, g,
             oacc, m_ref, l_tot);
@@ -558,7 +573,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
           oacc[dt][4 * i + e] = oacc[dt][4 * i + e] * a0 + v[e] * a1;
       }
   }
-  mend_row(row_ok, kp, a.k.row, vp, a.v.row, 32 * t0, min(lim + 1, 32 * t1), qf, g, oacc, m_ref, l_tot);
+  mend_row(row_ok, kp, a.k.row, vp, a.v.row, 32 * t0, min(lim + 1, 32 * t1), lim, min(Lk, 32 * t1), qf,
+           g, oacc, m_ref, l_tot);
   if (!row_ok) return;
   it.part += a.part0;
   write_row(a, a.splits + a.part0 > 1, it, (int64_t)a.B * a.nq * Hq, it.p0, tok, kvh * G + hg, Hq, g,
