@@ -59,8 +59,7 @@ const char* const kFamilyNames[] = {
     "attn_bwd_dkdv",  "attn_bwd_dq",   "gemm",           "gemm_wgrad",
     "reduce_splitk",  "lse_merge",     "rope",           "split_merge",
     "norm_rope",      "norm_rope_bwd", "norm_dw_fold",   "rows_fwd",
-    "rows_merge",     "rows_terms",    "rows_dkdv",      "rows_dkdv_fold",
-    "rows_dq",
+    "rows_merge",     "rows_dkdv",     "rows_dkdv_fold", "rows_dq",
 };
 const int kNumFamilies = sizeof(kFamilyNames) / sizeof(kFamilyNames[0]);
 

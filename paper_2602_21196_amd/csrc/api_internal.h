@@ -35,7 +35,6 @@ enum Family {
   kNormDwFold,
   kRowsFwd,
   kRowsMerge,
-  kRowsTerms,
   kRowsDkdv,
   kRowsDkdvFold,
   kRowsDq,

@@ -273,7 +273,6 @@ struct Plan {
   PlanHeader h{};
   std::vector<RowItem> fwd;
   std::vector<MergeItem> merge;
-  std::vector<TileItem> terms;
   std::vector<KeyItem> keys;
   std::vector<FoldItem> folds;
   std::vector<TileItem> dqs;
@@ -330,11 +329,7 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   longest_first(&fwd, &p->fwd);
 
   const int tpt = tile_tokens(G);
-  for (const Lengths& s : seqs) {
-    for (int t = 0; t < (s.Lq + tpt - 1) / tpt; ++t)
-      p->terms.push_back({s.q0, s.k0, h.term_rows, s.Lq, s.Lk, t, 0});
-    h.term_rows += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
-  }
+  for (const Lengths& s : seqs) h.term_rows += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
   std::vector<std::pair<int, KeyItem>> keys;
   each_key(seqs, G, causal, choose_segment(seqs, G, Hkv, causal),
            [&](int i, int64_t r0, int kb, int seg, int segs, int first, int count) {
@@ -357,17 +352,15 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   longest_first(&dqs, &p->dqs);
 
   auto fits = [&](size_t items, int threads) { return grid_fits((int64_t)items * Hkv, threads); };
-  if (!fits(p->fwd.size(), 512) || !fits(p->merge.size(), 256) || !fits(p->terms.size() * 4, 256) ||
+  if (!fits(p->fwd.size(), 512) || !fits(p->merge.size(), 256) ||
       !fits(p->keys.size(), 256) || !fits(p->folds.size() * 16, 256) || !fits(p->dqs.size(), 512))
     return UPIPE_ERR_UNSUPPORTED;
   h.n_fwd = (int32_t)p->fwd.size();
   h.n_merge = (int32_t)p->merge.size();
-  h.n_term = (int32_t)p->terms.size();
   h.n_key = (int32_t)p->keys.size();
   h.n_fold = (int32_t)p->folds.size();
   h.n_dq = (int32_t)p->dqs.size();
   int64_t end = round_up(sizeof(PlanHeader), 64);
-  h.at_term = place(&end, p->terms);
   h.at_key = place(&end, p->keys);
   h.at_fold = place(&end, p->folds);
   h.at_dq = place(&end, p->dqs);
@@ -444,7 +437,6 @@ int upipe_varlen_plan(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int H
     memcpy(to, &p.h, sizeof(p.h));
     put(to, p.h.at_fwd, p.fwd);
     put(to, p.h.at_merge, p.merge);
-    put(to, p.h.at_term, p.terms);
     put(to, p.h.at_key, p.keys);
     put(to, p.h.at_fold, p.folds);
     put(to, p.h.at_dq, p.dqs);
@@ -568,14 +560,12 @@ int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
     a.lse_c = a.D + Hkv * h->term_rows;
     a.sums = (float*)((char*)ws + sums_at(*h));
     a.slots = h->slots;
-    a.terms = (const TileItem*)(dev + h->at_term);
     a.keys = (const KeyItem*)(dev + h->at_key);
     a.folds = (const FoldItem*)(dev + h->at_fold);
     a.dqs = (const TileItem*)(dev + h->at_dq);
     a.Hkv = Hkv;
     a.G = G;
     a.causal = h->causal;
-    if (h->n_term > 0) UPIPE_LAUNCH(kRowsTerms, stream, launch_rows_terms(a, h->n_term, stream));
     if (h->n_dq > 0) UPIPE_LAUNCH(kRowsDq, stream, launch_rows_dq(h->dq_ks, a, h->n_dq, stream));
     if (h->n_key > 0) UPIPE_LAUNCH(kRowsDkdv, stream, launch_rows_dkdv(a, h->n_key, stream));
     if (h->n_fold > 0)

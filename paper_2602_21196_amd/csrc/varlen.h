@@ -40,7 +40,7 @@ struct FoldItem {
   int64_t k0;
   int32_t Lk, kb, slot, n;
 };
-// Tile `tile` of a sequence's packed rows: of 128 for the row terms, of dQ's own size.
+// Tile `tile` of a sequence's packed rows for dQ.
 struct TileItem {
   int64_t q0, k0, r0;
   int32_t Lq, Lk, tile, pad;
@@ -57,8 +57,8 @@ struct PlanHeader {
   int32_t n_seq, Hq, Hkv, causal;
   int32_t fwd_ks, dq_ks;               // key parts inside a workgroup
   int32_t parts;                       // the most of a row
-  int32_t n_fwd, n_merge, n_key, n_fold, n_term, n_dq;
-  int64_t at_fwd, at_merge, at_key, at_fold, at_term, at_dq;     // byte offsets
+  int32_t n_fwd, n_merge, n_key, n_fold, n_dq;
+  int64_t at_fwd, at_merge, at_key, at_fold, at_dq;     // byte offsets
 };
 
 // Query tokens of a 128-row tile of the backward.
@@ -106,19 +106,17 @@ struct RowBwdArgs {
   const float* lse;
   int64_t lse_head;
   // Row terms [Hkv][term_rows]: D = dO.o and -sqrt(d) lse of the packed rows, in tiles
-  // of 128 rows, tile_tokens(G) G of them used.
+  // of 128 rows, tile_tokens(G) G of them used.  dQ leaves them for dK/dV.
   float *D, *lse_c;
   int64_t term_rows;
   float* sums;               // [Hkv][slots][2][128][128] sums of segments
   int64_t slots;
-  const TileItem* terms;
   const KeyItem* keys;
   const FoldItem* folds;
   const TileItem* dqs;
   int Hkv, G, causal;
 };
 // n items of every key/value head.
-hipError_t launch_rows_terms(const RowBwdArgs& a, int64_t n, hipStream_t st);
 hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st);
 hipError_t launch_rows_dkdv_fold(const RowBwdArgs& a, int64_t n, hipStream_t st);
 hipError_t launch_rows_dq(int ks, const RowBwdArgs& a, int64_t n, hipStream_t st);

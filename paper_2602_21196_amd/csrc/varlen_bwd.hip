@@ -7,8 +7,8 @@
 // products (as the matrix instructions take them), all sums are fp32.  The rows of
 // a key/value group are packed (varlen.h), so dK and dV sum over the group's heads by
 // walking its rows.  No atomics: every sum has a fixed order.
-//   terms: D and -sqrt(d) lse of the packed rows, in tiles of 128
-//   dq:    a workgroup owns 256, 128 or 64 packed rows and walks stages of keys
+//   dq:    a workgroup owns 256, 128 or 64 packed rows, forms their terms, D and
+//          -sqrt(d) lse, which it leaves for dkdv, and walks stages of keys
 //   dkdv:  a workgroup owns 128 keys of one key/value head and walks the tiles of
 //          rows that see them, from the last one down; long walks are cut into
 //          segments side by side, whose sums are added in their order
@@ -20,37 +20,6 @@
 namespace upipe {
 
 namespace {
-
-// 32 rows of one tile of 128; sixteen lanes a row.  Rows that see no key get zeros:
-// every pair of theirs is masked, and zeros keep what is masked finite.
-__global__ __launch_bounds__(256) void rows_terms_kernel(RowBwdArgs a) {
-  const int kvh = blockIdx.x / 4 % a.Hkv;
-  const TileItem it = a.terms[blockIdx.x / 4 / a.Hkv];
-  const int c = threadIdx.x & 15, G = a.G, tpt = tile_tokens(G);
-  const int64_t out = kvh * a.term_rows + it.r0 + it.tile * 128;
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int r = 32 * (blockIdx.x % 4) + 16 * i + (threadIdx.x >> 4);
-    const int t = r / G, tok = it.tile * tpt + t, h = kvh * G + r - t * G;
-    float acc = 0.f, l = -INFINITY;
-    if (t < tpt && tok < it.Lq) {
-      l = a.lse[h * a.lse_head + it.q0 + tok];
-      const bf16x8 x = *reinterpret_cast<const bf16x8*>(
-          a.dO.p + (it.q0 + tok) * a.dO.row + h * a.dO.head + 8 * c);
-      const bf16x8 y = *reinterpret_cast<const bf16x8*>(
-          a.o.p + (it.q0 + tok) * a.o.row + h * a.o.head + 8 * c);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc = fmaf((float)x[e], (float)y[e], acc);
-    }
-#pragma unroll
-    for (int off = 8; off >= 1; off >>= 1) acc += __shfl_xor(acc, off);
-    if (c == 0) {
-      const bool none = l == -INFINITY;
-      a.D[out + r] = none ? 0.f : acc;
-      a.lse_c[out + r] = none ? 0.f : l * -11.313708498984761f;     // -sqrt(128) lse
-    }
-  }
-}
 
 // ------------------------------------------------------------------ dK / dV
 // The copies of one tile by one wave, as the products' kernel wants them
@@ -162,8 +131,9 @@ __global__ __launch_bounds__(256, 1) void rows_dkdv_kernel(RowBwdArgs a) {
                         (INSIDE ? (next.tokens - 1) * q_row + q_in : 0x7fffffffu) & on);
     next.dO = rsrc_words(dh + tok * a.dO.row,
                          (INSIDE ? (next.tokens - 1) * d_row + d_in : 0x7fffffffu) & on);
-    next.lse = rsrc_words(lh + (int64_t)tile * QT, (QT * 4) & on);
-    next.D = rsrc_words(Dh + (int64_t)tile * QT, (QT * 4) & on);
+    // rows without a token have no terms: zeros
+    next.lse = rsrc_words(lh + (int64_t)tile * QT, (uint32_t)(next.tokens * G * 4) & on);
+    next.D = rsrc_words(Dh + (int64_t)tile * QT, (uint32_t)(next.tokens * G * 4) & on);
     next.lds = lds;
   };
   aim(it.first, it.count > 0, lds0);
@@ -349,22 +319,36 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
     for (int i = 0; i < T::BLK; i += 2) issue(rk, rv, i, lds0);
   }
 
-  auto term_of = [&](int tpt) {
-    return kvh * a.term_rows + it.r0 + (int64_t)(tok / tpt) * 128 + (tok % tpt) * G + hg;
+  // The row's terms: for dkdv too, in tiles of 128 rows.  A row that sees no key has zeros:
+  // every pair of its is masked, and zeros keep what is masked finite.
+  auto put_term = [&](float* to, float x) {
+    const int tpt = tile_tokens(G);
+    if (ks == 0 && g == 0 && rw + r32 < n_rows)
+      to[kvh * a.term_rows + it.r0 + (int64_t)(tok / tpt) * 128 + (tok % tpt) * G + hg] = x;
   };
+  const int lim = last_key(tok), lim_w = last_key(rw / G);
   bf16x8 qf[8], df[8];
-  float nlse, Dq;   // nlse = -sqrt(d) lse: the score accumulator's seed
+  float nlse, Dq = 0.f;   // nlse = -sqrt(d) lse: the score accumulator's seed
   {
-    const int h = kvh * G + hg, tpt = tile_tokens(G);
+    const int h = kvh * G + hg;
     const bf16* qp = a.q.p + (it.q0 + tok) * a.q.row + h * a.q.head + 8 * g;
     const bf16* dp = a.dO.p + (it.q0 + tok) * a.dO.row + h * a.dO.head + 8 * g;
+    const bf16* op = a.o.p + (it.q0 + tok) * a.o.row + h * a.o.head + 8 * g;
+    const float l = a.lse[h * a.lse_head + it.q0 + tok];
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s);
       df[s] = *reinterpret_cast<const bf16x8*>(dp + 16 * s);
+      const bf16x8 of = *reinterpret_cast<const bf16x8*>(op + 16 * s);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) Dq = fmaf((float)df[s][e], (float)of[e], Dq);
     }
-    nlse = a.lse_c[term_of(tpt)];
-    Dq = a.D[term_of(tpt)];
+    Dq += __shfl_xor(Dq, 32);
+    const bool none = l == -INFINITY;
+    nlse = none ? 0.f : l * -11.313708498984761f;     // -sqrt(128) lse
+    if (none) Dq = 0.f;
+    put_term(a.lse_c, nlse);
+    if (lim < 0 || lim >= kFewKeys) put_term(a.D, Dq);
   }
 
   f32x16 qacc[4];
@@ -377,7 +361,6 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
   const uint32_t k_lane = T::OFF_K + k_part * 256 + swzt(r32, g);
   const uint32_t v_lane = T::OFF_V + k_part * 256 + swzt(r32, g);
   const uint32_t t_lane = T::OFF_K + k_part * 256 + tr_base(lane);
-  const int lim = last_key(tok), lim_w = last_key(rw / G);
   // Stages with a key of this wave's part that a row of it may see come first.
   const int seen_w = last_key((min(rw + 32, n_rows) - 1) / G) + 1;
   const int nw = rw >= n_rows ? 0 : max(0, min(nst, (seen_w - k_part + T::BK - 1) / T::BK));
@@ -424,7 +407,7 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
         d += __shfl_xor(d, 32);
         if (lim >= 0 && lim < kFewKeys) {
           Dq = d;
-          if (g == 0 && rw + r32 < n_rows) a.D[term_of(tile_tokens(G))] = d;
+          put_term(a.D, d);
         }
       }
       float ds[16];
@@ -501,11 +484,6 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
 }
 
 }  // namespace
-
-hipError_t launch_rows_terms(const RowBwdArgs& a, int64_t n, hipStream_t st) {
-  hipLaunchKernelGGL(rows_terms_kernel, dim3((unsigned)(n * a.Hkv * 4)), dim3(256), 0, st, a);
-  return hipGetLastError();
-}
 
 hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st) {
   auto inside = [&](const HeadView& v) { return v.row >= (a.G - 1) * v.head + HEAD_DIM; };
