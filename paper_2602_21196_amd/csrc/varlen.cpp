@@ -60,10 +60,15 @@ struct Lengths {
 };
 
 // us of one 128-key stage of a forward workgroup with 1, 2, 4 key parts on a full
-// chip, and of a workgroup besides its stages.
+// chip, and of a workgroup besides its stages.  What they lead to, us with 1 | 2 | 4 (the
+// chosen one first): 64 documents of 256 tokens, 4 heads, 1: 21 | 28 | 43; 8192 tokens, 8
+// heads on 2, 2: 142 | 181 (1) | 174 (4); 16384, 8 heads, 1: 477 | 519 | 636; 2048 in
+// documents of up to 700, 4 heads, 4: 16 | 27 (1) | 18 (2).
 constexpr double kFwdStage[3] = {3.5, 2.0, 1.2}, kFwdFixed = 3.0;
 constexpr int kFwdParts[3] = {1, 2, 4};
-// us that a merge launch takes, and that it takes for one part of 64 rows.
+// us that a merge launch takes, and that it takes for one part of 64 rows.  16 queries of 8
+// heads on 50000 keys: in parts of 4 stages 18 + 5 us, of 16 26 + 5, whole 402; 500
+// queries on 16000 keys: parts of 8 stages 43 + 6, whole 134.
 constexpr double kMergeFixed = 4.0, kMergePart = 0.01;
 
 struct FwdChoice {
@@ -142,7 +147,10 @@ FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causa
 }
 
 // us of a dK/dV tile of 128 rows, of a workgroup besides its tiles, of the fold's
-// launch and of a segment's sums in it.
+// launch and of a segment's sums in it.  65536 tokens in documents of up to 32768, 8
+// heads on 1: segments of 512 tiles 4.91 ms, of 128 or 256 the same, 1024 5.07, whole
+// walks 7.22; 2048 tokens in documents of up to 700, 4 heads: 2 tiles 17 + 4 us, 1 tile
+// 14 + 6, 4 tiles 23 + 4, whole walks 75.
 constexpr double kKeyTile = 4.0, kKeyFixed = 8.0, kFoldFixed = 5.0, kFoldSum = 0.065;
 constexpr int64_t kMaxSums = 2048;     // segment sums of all heads: 256 MB of workspace
 
@@ -208,7 +216,9 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
   return best;
 }
 
-// us of a dQ stage with 1 (64 keys), 2 and 4 (128 keys) key parts on a full chip.
+// us of a dQ stage with 1 (64 keys), 2 and 4 (128 keys) key parts on a full chip.  us with
+// 1 | 2 | 4: 64 documents of 256 tokens, 4 heads 26 | 37 | 56; 8192 tokens, 8 heads on 2
+// 262 | 198 | 223; 2048 in documents of up to 700, 4 heads 34 | 24 | 20.
 constexpr double kDqStage[3] = {2.5, 2.8, 1.6}, kDqFixed = 4.0;
 
 // Calls f(sequence, r0, tile, stages) for every workgroup of dQ.
@@ -308,10 +318,15 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   h.fwd_ks = c.ks;
   // Partial rows: [parts][Lq][Hq] of every sequence that is cut.
   std::vector<int64_t> p0;
-  h.parts = 1;
-  for (const Lengths& s : seqs)
-    if (s.Lq > 0) h.parts = std::max(h.parts, seq_parts(s, c.most));
-  const int per_block = h.parts > kSomeParts ? 1 : 16;
+  int parts = 1;
+  int64_t merged = 0;
+  for (const Lengths& s : seqs) {
+    const int np = seq_parts(s, c.most);
+    if (np > 1) merged += (int64_t)s.Lq * Hq;
+    if (s.Lq > 0) parts = std::max(parts, np);
+  }
+  h.one_row = many_parts(parts, merged);
+  const int per_block = h.one_row ? 1 : 16;
   for (const Lengths& s : seqs) {
     const int np = seq_parts(s, c.most);
     p0.push_back(h.part_rows);
@@ -495,7 +510,7 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
       m.lse_head = lse_head;
       m.items = (const MergeItem*)((const char*)plan_dev + h->at_merge);
       m.Hq = Hq;
-      m.parts = h->parts;
+      m.one_row = h->one_row;
       UPIPE_LAUNCH(kRowsMerge, stream, launch_rows_merge(m, h->n_merge, stream));
     }
     return UPIPE_OK;
@@ -600,9 +615,38 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
   return grid_fits(B * nq * Hq, 512) ? UPIPE_OK : UPIPE_ERR_UNSUPPORTED;
 }
 
+// The prefix's workgroups: 256, 128 or 64 packed rows (1, 2 or 4 key parts inside)
+// against one of `parts` parts of it, expected to end first.  us of a stage and of a
+// workgroup besides (its rows of 16384 x 8 heads, 64 a sequence, 1 | 2 | 4: 64 sequences
+// 42 | 42 | 47 us, 256 sequences 142 | 150 | 179, 64 of one head of 8 rows 20 | 18 | 15).
+constexpr double kPrefixStage[3] = {4.2, 2.25, 1.3}, kPrefixFixed = 8.0;
+
+void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
+  const int64_t stages = (P + 127) / 128;
+  double best = 0.0;
+  for (int i = 0; i < 3; ++i) {
+    const int64_t n = (rows * kFwdParts[i] + 255) / 256 * Hkv;
+    for (int64_t parts = 1; parts <= std::min<int64_t>(stages, 2 * kCUs); ++parts) {
+      const int64_t rounds = (n * parts + kCUs - 1) / kCUs;
+      const double est = rounds * (kPrefixFixed + (stages + parts - 1) / parts * kPrefixStage[i]) +
+                         kMergePart * n * parts * (4.0 / kFwdParts[i]);
+      if (best == 0.0 || est < best) {
+        best = est;
+        p->prefix_ks = kFwdParts[i];
+        p->prefix_parts = (int)parts;
+      }
+      if (rounds > 4) break;
+    }
+  }
+}
+
 // The lengths are on the device: the cut goes by the capacity, and a part is the
 // same share of whatever a cache holds.  About four workgroups a CU even out caches of
-// different lengths.
+// different lengths (24 of 1 to 16384 rows, 8 heads: 1 | 2 | 4 | 8 a CU 176 | 145 |
+// 110 | 110 us), of 512 rows at least (131072 rows of one cache, parts of 256 | 512 |
+// 1024: 48 | 37 | 33 us before the merge had its loads under way together, 23 with 512).
+// Up to 32 packed rows a cache goes by few_rows_kernel (64 caches of 512 rows, 8 heads of
+// 8 rows: 25 us, by the tiles of 64 rows 37; one of 131071 rows 16.5 and 17).
 CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv) {
   CachePlan p;
   p.rows = B * nq * Hq;
@@ -611,12 +655,7 @@ CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv)
   const int64_t groups = B * Hkv * (p.few ? 1 : (nq * G + 63) / 64);
   const int64_t least = (cap + 511) / 512;      // parts of 512 rows
   p.splits = (int)std::max<int64_t>(1, std::min((4 * kCUs + groups - 1) / groups, least));
-  if (P > 0) {
-    const int64_t rows = B * nq * G, ps = (P + 127) / 128;
-    p.prefix_ks = rows > 128 ? 1 : rows > 64 ? 2 : 4;
-    const int64_t n = (rows * p.prefix_ks + 255) / 256 * Hkv;
-    p.prefix_parts = (int)std::max<int64_t>(1, std::min((kCUs + n - 1) / n, (ps + 1) / 2));
-  }
+  if (P > 0) plan_prefix(B * nq * G, P, Hkv, &p);
   return p;
 }
 
@@ -630,6 +669,8 @@ bool apart_cache(const upipe_heads& o, int64_t T, int Hq, const upipe_heads& k, 
 
 int64_t cache_parts(const CachePlan& p) { return p.splits + p.prefix_parts; }
 
+size_t cache_ws(const CachePlan& p) { return parts_bytes(cache_parts(p) * p.rows) + 16; }
+
 }  // namespace
 
 }  // namespace upipe
@@ -639,8 +680,7 @@ extern "C" {
 size_t upipe_attn_decode_workspace_size(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv,
                                         int d) {
   if (check_cache(B, nq, cap, P, Hq, Hkv, d) != UPIPE_OK) return 0;
-  const CachePlan p = plan_cache(B, nq, cap, P, Hq, Hkv);
-  return parts_bytes(cache_parts(p) * p.rows) + 16;
+  return cache_ws(plan_cache(B, nq, cap, P, Hq, Hkv));
 }
 
 int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads v, int64_t v_cache,
@@ -665,9 +705,8 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
       return UPIPE_ERR_INVALID_ARG;
     if (!stage_rows(k) || !stage_rows(v) || (P > 0 && (!stage_rows(k_prefix) || !stage_rows(v_prefix))))
       return UPIPE_ERR_UNSUPPORTED;
-    if (ws_bytes < upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d))
-      return UPIPE_ERR_WORKSPACE;
     const CachePlan p = plan_cache(B, nq, cap, P, Hq, Hkv);
+    if (ws_bytes < cache_ws(p)) return UPIPE_ERR_WORKSPACE;
     const int G = Hq / Hkv;
     RowFwdArgs a{};
     a.q = view_of(q);
@@ -715,6 +754,7 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     m.rows = p.rows;
     m.Hq = Hq;
     m.parts = (int)cache_parts(p);
+    m.one_row = many_parts(m.parts, m.rows);
     m.nq = nq;
     UPIPE_LAUNCH(kRowsMerge, stream, launch_rows_merge(m, 0, stream));
     return UPIPE_OK;

@@ -21,9 +21,14 @@ struct RowItem {
   int32_t Lq, Lk;
   int32_t tile, part, parts, pad;
 };
-// 16 rows of a sequence whose parts are merged, or, where some row has more than
-// kSomeParts, one.
+// 16 rows of a sequence whose parts are merged, or, with many_parts, one.
 constexpr int kSomeParts = 64, kMostParts = 2048;
+// Whether a workgroup merges one row (else 16): with many parts, or few rows of some.  us,
+// two events among them, 16 rows | one: 8 rows of 16 parts 6.9 | 7.0, of 32 8.7 | 6.9; 768
+// rows of 16 8.7 | 8.6, of 32 11.7 | 9.4; 2048 rows of 32 13.0 | 16.5, of 64 20.5 | 20.8.
+inline bool many_parts(int parts, int64_t rows) {
+  return parts > kSomeParts || (parts > 16 && rows < 1024);
+}
 struct MergeItem {
   int64_t q0, p0;
   int32_t Lq, parts, block, pad;
@@ -56,7 +61,7 @@ struct PlanHeader {
   int64_t longest_q, longest_k;
   int32_t n_seq, Hq, Hkv, causal;
   int32_t fwd_ks, dq_ks;               // key parts inside a workgroup
-  int32_t parts;                       // the most of a row
+  int32_t one_row;                     // of a merging workgroup
   int32_t n_fwd, n_merge, n_key, n_fold, n_dq;
   int64_t at_fwd, at_merge, at_key, at_fold, at_dq;     // byte offsets
 };
@@ -92,12 +97,9 @@ struct RowMergeArgs {
   const MergeItem* items;    // planned sequences; else all rows of B caches
   int64_t rows;              // B * nq * Hq
   int Hq, nq;
-  int parts;                 // planned: the most of a row
+  int parts;                 // not planned
+  bool one_row;              // many_parts
 };
-// Whether a workgroup merges one row (else 16): with many parts, or few rows of some.
-inline bool many_parts(int parts, int64_t rows) {
-  return parts > kSomeParts || (parts > 8 && rows < 1024);
-}
 hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t items, hipStream_t st);
 
 // ---- backward (varlen_bwd.hip) ---------------------------------------------

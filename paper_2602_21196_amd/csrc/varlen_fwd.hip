@@ -12,6 +12,11 @@
 //     workgroup's waves: 256, 128 or 64 rows;
 //   - one launch over a host-made list of tiles, longest first;
 //   - a tile's keys cut into parts where tiles are few: fp32 results, merged.
+// Up to 32 packed rows a cache have a kernel of their own (few_rows_kernel).
+// What bounds it: MFMA issue where tiles fill the chip (131072 tokens, 4 heads on 1: 14.2
+// ms, 1240 TFLOP/s, as the forward over equal lengths; 65536 tokens in documents of up to
+// 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 110 us,
+// 4.6 TB/s; a plain read of as much 5.4), launches and one chain of stages in short calls.
 #include "varlen.h"
 
 namespace upipe {
@@ -46,12 +51,12 @@ __device__ __forceinline__ float tile_probs(const f32x16 (&st)[NT], bf16x8 (&pf)
 
 // One stage for one wave: the 32 NT keys from key kb on.  k_at and v_at: this lane's
 // place of the first key's chunk g and of its transposing reads of V (common.h); the
-// others are exclusive-ors of them (a register for each would spill).  This lane's row sees the keys up to `lim`, the wave's first row
-// those up to lim_w.  copy_k and copy_v issue the next stage's copies.
+// others are exclusive-ors of them (a register for each would spill).  This lane's row
+// sees the keys up to `lim`, the wave's first row those up to lim_w.  copy_k and copy_v
+// issue the next stage's copies.
 template <int NT, class CopyK, class CopyV>
 __device__ __forceinline__ void fwd_stage(const char* smem, uint32_t k_at, uint32_t v_at, int kb,
-                                          int lane,
-                                          const bf16x8 (&qf)[8], int lim, int lim_w,
+                                          int lane, const bf16x8 (&qf)[8], int lim, int lim_w,
                                           f32x16 (&oacc)[4], float& m_ref, float& l_run,
                                           const CopyK& copy_k, const CopyV& copy_v) {
   const float sl2 = 1.4426950408889634f * 0.08838834764831845f;  // log2(e)/sqrt(128)
@@ -78,9 +83,9 @@ __device__ __forceinline__ void fwd_stage(const char* smem, uint32_t k_at, uint3
   __builtin_amdgcn_sched_group_barrier(0x008, 6, 0);
   // The next stage's copies follow the two blocks of products they can hide
   // behind: a wave stands still while the CU takes them, and at the top of
-  // the stage nothing of it is under way.  Against there: one head over 4096
-  // keys 43 -> 39 us, 8 heads over 4096 56 -> 52, 4 over 8192 90 -> 86, long
-  // calls, where other waves fill the gap, within 0.5 %.
+  // the stage nothing of it is under way.  Against there, in the forward over equal
+  // lengths: one head over 4096 keys 43 -> 39 us, 4 over 8192 90 -> 86, long calls,
+  // where other waves fill the gap, within 0.5 %.
   copy_k();
   // Mask keys past the row's last visible key (wave-uniform test first).
   if (kb + 32 * NT - 1 > lim_w) {
@@ -179,13 +184,13 @@ __device__ __forceinline__ void fold_in(const char* smem, int wq, int lane, f32x
   }
 }
 
-
 // A row against its keys by plain arithmetic.  The lane pair of a row has its query and
 // output elements as the tile has them.  Ends early once a visible score is not a
 // number, or no element is finite any more: so it stays.
-__device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const bf16* v, int64_t v_row,
-                                         int64_t key0, int64_t key1, const bf16x8 (&qf)[8], int g,
-                                         f32x16 (&oacc)[4], float& m_ref, float& l) {
+__device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const bf16* v,
+                                            int64_t v_row, int64_t key0, int64_t key1,
+                                            const bf16x8 (&qf)[8], int g, f32x16 (&oacc)[4],
+                                            float& m_ref, float& l) {
   const float sl2 = 1.4426950408889634f * 0.08838834764831845f;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
@@ -417,8 +422,8 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
       copy4_b128(nv, offv, 0, nlds + K_TILE);
       continue;
     }
-    fwd_stage<NT>(smem, k_lane + boff, v_lane + boff, j * BKS + k_part, lane, qf, lim, lim_w, oacc, m_ref, l_run,
-                  [&]() { copy4_b128(nk, offk, 0, nlds); },
+    fwd_stage<NT>(smem, k_lane + boff, v_lane + boff, j * BKS + k_part, lane, qf, lim, lim_w, oacc,
+                  m_ref, l_run, [&]() { copy4_b128(nk, offk, 0, nlds); },
                   [&]() { copy4_b128(nv, offv, 0, nlds + K_TILE); });
   }
 
@@ -442,8 +447,9 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
   mend_row(row_ok, kp, a.k.row, vp, a.v.row, j0 * BKS, min(lim + 1, j1 * BKS), lim,
            min(it.Lk, min(j1, (seen_w + BKS - 1) / BKS) * BKS), qf, g, oacc, m_ref, l_tot);
   if (!row_ok) return;
-  write_row(a, MODE == kRowsOne || (MODE == kRowsCache ? a.splits + a.part0 : it.parts) > 1, it, part_rows, lse_at, tok, kvh * G + hg, Hq, g,
-            oacc, m_ref, l_tot);
+  const bool part =
+      MODE == kRowsOne || (MODE == kRowsCache ? a.splits + a.part0 : it.parts) > 1;
+  write_row(a, part, it, part_rows, lse_at, tok, kvh * G + hg, Hq, g, oacc, m_ref, l_tot);
 }
 
 // Up to 32 packed rows of one cache and key/value head: a wave takes every NW-th 32-key
@@ -528,8 +534,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
     const uint32_t boff = (w * 4 + 2 * (n & 1)) * kFewTile;
     // This tile's 16 copies have landed; the next one's may be under way.
     asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-    fwd_stage<1>(smem, k_lane + boff, v_lane + boff, 32 * t, lane, qf, lim, lim_w, oacc, m_ref, l_run,
-                 []() {}, []() {});
+    fwd_stage<1>(smem, k_lane + boff, v_lane + boff, 32 * t, lane, qf, lim, lim_w, oacc, m_ref,
+                 l_run, []() {}, []() {});
     // Every read of the tile is done: its place takes the copies of the next but one.
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     copy(t + 2 * kFewWaves, lds_address(smem) + boff);
@@ -573,12 +579,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
           oacc[dt][4 * i + e] = oacc[dt][4 * i + e] * a0 + v[e] * a1;
       }
   }
-  mend_row(row_ok, kp, a.k.row, vp, a.v.row, 32 * t0, min(lim + 1, 32 * t1), lim, min(Lk, 32 * t1), qf,
-           g, oacc, m_ref, l_tot);
+  mend_row(row_ok, kp, a.k.row, vp, a.v.row, 32 * t0, min(lim + 1, 32 * t1), lim,
+           min(Lk, 32 * t1), qf, g, oacc, m_ref, l_tot);
   if (!row_ok) return;
   it.part += a.part0;
-  write_row(a, a.splits + a.part0 > 1, it, (int64_t)a.B * a.nq * Hq, it.p0, tok, kvh * G + hg, Hq, g,
-            oacc, m_ref, l_tot);
+  write_row(a, a.splits + a.part0 > 1, it, (int64_t)a.B * a.nq * Hq, it.p0, tok, kvh * G + hg,
+            Hq, g, oacc, m_ref, l_tot);
 }
 
 // The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
@@ -724,15 +730,14 @@ hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t 
 }
 
 hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t items, hipStream_t st) {
-  const bool many = a.items != nullptr ? a.parts > kSomeParts : many_parts(a.parts, a.rows);
-  const int64_t blocks = a.items != nullptr ? items : many ? a.rows : (a.rows + 15) / 16;
+  const int64_t blocks = a.items != nullptr ? items : a.one_row ? a.rows : (a.rows + 15) / 16;
 #define UPIPE_MERGE(GP, P) \
   hipLaunchKernelGGL((rows_merge_kernel<GP, P>), dim3((unsigned)blocks), dim3(256), 0, st, a)
   if (a.items != nullptr) {
-    if (many) UPIPE_MERGE(16, true);
+    if (a.one_row) UPIPE_MERGE(16, true);
     else UPIPE_MERGE(1, true);
   } else {
-    if (many) UPIPE_MERGE(16, false);
+    if (a.one_row) UPIPE_MERGE(16, false);
     else UPIPE_MERGE(1, false);
   }
 #undef UPIPE_MERGE
