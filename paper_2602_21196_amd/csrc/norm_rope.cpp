@@ -39,8 +39,9 @@ int norm_args(const upipe_heads& q, const upipe_heads& k, const void* wq, const 
   a->k.w = wk;
   a->q.H = Hq;
   a->k.H = Hkv;
+  const double log2_base = std::log2(base);
   for (int e = 0; e < HEAD_DIM / 2; ++e)
-    a->freq.turns[e] = std::exp2(-(double)e * std::log2(base) / 64.0) * 0.15915494309189535;
+    a->freq.turns[e] = std::exp2(-(double)e * log2_base / 64.0) * 0.15915494309189535;
   a->positions = positions;
   a->T = T;
   a->eps = (float)eps;

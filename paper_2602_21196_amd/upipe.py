@@ -338,9 +338,15 @@ def upipe_profile_names():
 
 # ------------------------------------------------------ torch conveniences
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _ptr(t, dtype, name):
@@ -640,22 +646,24 @@ def _rows(t, name, shape=None):
     return upipe_heads(t.data_ptr(), stride[0] if T > 1 else H * head, head)
 
 
-def _call(fn, args, **tensors):
+def _call(fn, args, *tensors):
     """lib().fn(*args, stream) on the current stream of the tensors' device, made the
-    current one; all of them have to be on it."""
-    it = iter(tensors.values())
-    dev = next(it).get_device()
-    for t in it:
+    current one; all of them (None: not given) have to be on it."""
+    dev = tensors[0].get_device()
+    for t in tensors:
         if t is not None and t.get_device() != dev:
-            raise ValueError("tensors on different devices: " + ", ".join(
-                f"{n} on {t.device}" for n, t in tensors.items() if t is not None))
-    cuda = _torch().cuda
-    if cuda.current_device() == dev:
-        st = getattr(lib(), fn)(*args, cuda.current_stream().cuda_stream)
+            raise ValueError(f"{fn}: tensors on different devices: " + ", ".join(
+                str(t.device) for t in tensors if t is not None))
+    torch = _torch()
+    # the stream's handle; current_stream().cuda_stream makes an object of it first (2.5 us)
+    stream = torch._C._cuda_getCurrentRawStream(dev)
+    if torch.cuda.current_device() == dev:
+        st = getattr(lib(), fn)(*args, stream)
     else:
-        with cuda.device(dev):
-            st = getattr(lib(), fn)(*args, cuda.current_stream().cuda_stream)
-    _check(fn, st)
+        with torch.cuda.device(dev):
+            st = getattr(lib(), fn)(*args, stream)
+    if st != UPIPE_OK:
+        raise UpipeError(fn, st)
 
 
 def _workspace(ws, need, device, fn):
@@ -686,13 +694,12 @@ def _norm_inputs(q, k, wq, wk, positions):
              int(wq.dtype == torch.float32), _ptr(positions, torch.int64, "positions")))
 
 
-def _pair_out(out, shapes, device, names):
-    """The caller's two output tensors, or two new dense ones."""
+def _pair_out(out, q, k, names):
+    """The caller's two output tensors, like q and k, or two new dense ones."""
     if out is None:
-        torch = _torch()
-        return tuple(torch.empty(s, dtype=torch.bfloat16, device=device) for s in shapes)
-    for t, s, n in zip(out, shapes, names):
-        _rows(t, n, s)
+        return q.new_empty(q.shape), k.new_empty(k.shape)
+    for t, like, n in zip(out, (q, k), names):
+        _rows(t, n, like.shape)
     return tuple(out)
 
 
@@ -701,11 +708,11 @@ def qk_norm_rope(q, k, wq, wk, positions, base, eps=1e-6, out=None):
     elements, times wq / wk [d] (bf16 or fp32), rotated at positions [T] (int64).
     q, k and out = (q', k') may be strided views with dense rows; out may be (q, k)."""
     T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
-    yq, yk = _pair_out(out, (tuple(q.shape), tuple(k.shape)), q.device, ("q_out", "k_out"))
+    yq, yk = _pair_out(out, q, k, ("q_out", "k_out"))
     _call("upipe_qk_norm_rope",
           (vq, vk, *rest, _rows(yq, "q_out"), _rows(yk, "k_out"), T, Hq, Hkv, q.shape[2],
            float(base), float(eps)),
-          q=q, k=k, wq=wq, wk=wk, positions=positions, q_out=yq, k_out=yk)
+          q, k, wq, wk, positions, yq, yk)
     return yq, yk
 
 
@@ -715,7 +722,7 @@ def qk_norm_rope_bwd(q, k, wq, wk, positions, base, dq_out, dk_out, eps=1e-6, ou
     torch = _torch()
     T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
     vdq, vdk = _rows(dq_out, "dq_out", q.shape), _rows(dk_out, "dk_out", k.shape)
-    dq, dk = _pair_out(out, (tuple(q.shape), tuple(k.shape)), q.device, ("dq", "dk"))
+    dq, dk = _pair_out(out, q, k, ("dq", "dk"))
     dwq, dwk = torch.empty_like(wq), torch.empty_like(wk)
     ws = _workspace(ws, upipe_qk_norm_rope_bwd_workspace_size(T, Hq, Hkv, q.shape[2]), q.device,
                     "upipe_qk_norm_rope_bwd_workspace_size")
@@ -723,8 +730,7 @@ def qk_norm_rope_bwd(q, k, wq, wk, positions, base, dq_out, dk_out, eps=1e-6, ou
           (vq, vk, *rest, vdq, vdk, _rows(dq, "dq"), _rows(dk, "dk"), dwq.data_ptr(),
            dwk.data_ptr(), T, Hq, Hkv, q.shape[2], float(base), float(eps), ws.data_ptr(),
            ws.numel()),
-          q=q, k=k, wq=wq, wk=wk, positions=positions, dq_out=dq_out, dk_out=dk_out, dq=dq, dk=dk,
-          ws=ws)
+          q, k, wq, wk, positions, dq_out, dk_out, dq, dk, ws)
     return dq, dk, dwq, dwk
 
 
@@ -793,8 +799,8 @@ def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv))
     if out is None:
-        o = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-        lse = torch.empty((plan.Hq, q.shape[0]), dtype=torch.float32, device=q.device)
+        o = q.new_empty(q.shape)
+        lse = q.new_empty((plan.Hq, q.shape[0]), dtype=torch.float32)
         if Tq < q.shape[0]:
             o[Tq:] = 0
             lse[:, Tq:] = float("-inf")
@@ -804,7 +810,7 @@ def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
     _call("upipe_attn_fwd_varlen",
           (*views, _packed(o, "o", Tq, plan.Hq), *_packed_lse(lse, q, plan), plan.host,
            plan.dev.data_ptr(), ws.data_ptr(), ws.numel()),
-          q=q, k=k, v=v, o=o, lse=lse, plan=plan.dev, ws=ws)
+          q, k, v, o, lse, plan.dev, ws)
     return o, lse
 
 
@@ -817,7 +823,7 @@ def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv), _packed(o, "o", Tq, plan.Hq))
     if out is None:
-        out = tuple(torch.empty(t.shape, dtype=torch.bfloat16, device=q.device) for t in (q, k, v))
+        out = tuple(t.new_empty(t.shape) for t in (q, k, v))
         for t, n in zip(out, (Tq, Tk, Tk)):
             if n < t.shape[0]:
                 t[n:] = 0
@@ -828,7 +834,7 @@ def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     _call("upipe_attn_bwd_varlen",
           (*views, *_packed_lse(lse, q, plan), *grads, plan.host, plan.dev.data_ptr(),
            ws.data_ptr(), ws.numel()),
-          q=q, k=k, v=v, o=o, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, plan=plan.dev, ws=ws)
+          q, k, v, o, lse, dout, dq, dk, dv, plan.dev, ws)
     return dq, dk, dv
 
 
@@ -877,8 +883,8 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
         vkp = _rows(k_prefix, "k_prefix", (P, Hkv, d))
         vvp = _rows(v_prefix, "v_prefix", (P, Hkv, d))
     if out is None:
-        o = torch.empty((B, nq, Hq, d), dtype=torch.bfloat16, device=q.device)
-        lse = torch.empty((B, Hq, nq), dtype=torch.float32, device=q.device)
+        o = q.new_empty(q.shape)
+        lse = q.new_empty((B, Hq, nq), dtype=torch.float32)
     else:
         o, lse = out
         _shape(o, q.shape, "o")
@@ -889,8 +895,7 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
           (vq, vk, k_step, vv, v_step, _ptr(lens, torch.int32, "lens"), vkp, vvp,
            _rows(_flat_tokens(o, "o"), "o"), _ptr(lse, torch.float32, "lse"), B, nq, cap, P, Hq,
            Hkv, d, ws.data_ptr(), ws.numel()),
-          q=q, k_cache=k_cache, v_cache=v_cache, lens=lens, k_prefix=k_prefix, v_prefix=v_prefix,
-          o=o, lse=lse, ws=ws)
+          q, k_cache, v_cache, lens, k_prefix, v_prefix, o, lse, ws)
     return o, lse
 
 
