@@ -109,8 +109,7 @@ void each_fwd(const std::vector<Lengths>& seqs, int G, int causal, const FwdChoi
 }
 
 // The split of waves (1, 2 or 4 parts of a stage's keys) and of keys over
-// workgroups whose list is expected to end first.  Long lists need no look: from 16
-// workgroups a CU on the largest tiles are the fastest.
+// workgroups whose list is expected to end first.
 FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
   FwdChoice best;
   std::vector<int> units;
@@ -303,16 +302,11 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   const int G = Hq / Hkv;
   PlanHeader& h = p->h;
   h.magic = kPlanMagic;
-  h.n_seq = n;
   h.Hq = Hq;
   h.Hkv = Hkv;
   h.causal = causal;
   h.total_q = cu_q[n];
   h.total_k = cu_k[n];
-  for (const Lengths& s : seqs) {
-    h.longest_q = std::max<int64_t>(h.longest_q, s.Lq);
-    h.longest_k = std::max<int64_t>(h.longest_k, s.Lk);
-  }
 
   const FwdChoice c = choose_fwd(seqs, G, Hkv, causal);
   h.fwd_ks = c.ks;

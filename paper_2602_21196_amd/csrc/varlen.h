@@ -58,8 +58,7 @@ struct PlanHeader {
   int64_t part_rows;                   // fp32 partial rows of the forward
   int64_t term_rows;                   // row terms of one key/value head
   int64_t slots;                       // segment sums of one key/value head
-  int64_t longest_q, longest_k;
-  int32_t n_seq, Hq, Hkv, causal;
+  int32_t Hq, Hkv, causal;
   int32_t fwd_ks, dq_ks;               // key parts inside a workgroup
   int32_t one_row;                     // of a merging workgroup
   int32_t n_fwd, n_merge, n_key, n_fold, n_dq;

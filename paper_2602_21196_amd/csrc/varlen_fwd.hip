@@ -28,6 +28,10 @@ constexpr int K_TILE = BKS * HEAD_DIM * 2;       // [128][128] bf16 = 32 KB
 constexpr int V_TILE = HEAD_DIM * BKS * 2;       // [128][128] bf16 = 32 KB
 constexpr int STAGE = K_TILE + V_TILE;
 constexpr float kSumMax = 256.f;   // lazy-rescale bound on a lane's stage sum (2^8)
+// Reference max of a row before its first key (log2 domain): a finite stand-in for
+// -inf, below every finite score times log2(e) / sqrt(d), so that a stage whose keys are
+// all masked leaves the row at p = 0 rather than producing 0 * inf.
+constexpr float kNoMax = -3e38f;
 
 // P of a stage as the bf16 operand of P . V (one rounding of 2^-9 a weight, as the
 // matrix instructions take it), and this lane's sum of it in fp32, before that
@@ -196,7 +200,7 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-  m_ref = -1e30f;
+  m_ref = kNoMax;
   l = 0.f;
   for (int64_t j = key0; j < key1; ++j) {
     const bf16* kp = k + j * k_row + 8 * g;
@@ -208,6 +212,7 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
       for (int e = 0; e < 8; ++e) s = fmaf((float)kk[e], (float)qf[c][e], s);
     }
     s = (s + __shfl_xor(s, 32)) * sl2;
+    asm volatile("" : "+v"(s));      // rounded, as the maximum is: not fused with it
     const float m_new = fmaxf(m_ref, s), alpha = fast_exp2(m_ref - m_new);
     const float p = fast_exp2(s - m_new);
     m_ref = m_new;
@@ -235,7 +240,9 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
 // A masked key's weight is 0, but the matrix instructions also multiply that 0 by the
 // key's value, which may be infinite or not a number: then the rows of its stage come
 // out as NaN.  Such a row is formed again without it.  `lim`: the row's last key, `end`:
-// the end of the keys that its tile multiplied.
+// the end of the keys that its tile multiplied.  So is a row of scores beyond 2^30:
+// there the rounding of their maximum, which the stages' fused multiply-adds see, is
+// more than exp2 spans.
 __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_row, const bf16* v,
                                          int64_t v_row, int key0, int key1, int lim, int end,
                                          const bf16x8 (&qf)[8], int g, f32x16 (&oacc)[4],
@@ -246,9 +253,10 @@ __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_r
 #pragma unroll
     for (int i = 0; i < 16; ++i) z = fmaf(oacc[dt][i], 0.f, z);
   z += __shfl_xor(z, 32);
-  if (!row_ok || z == z) return;      // both lanes of a row alike
-  z = 0.f;
-  for (int j = max(lim + 1, key0); j < end; ++j) {
+  const bool far = m_ref != kNoMax && fabsf(m_ref) > 1073741824.f;
+  if (!row_ok || (z == z && !far)) return;      // both lanes of a row alike
+  z = far ? NAN : 0.f;
+  for (int j = max(lim + 1, key0); j < end && !far; ++j) {
     const bf16* p = v + j * v_row + 64 * g;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -404,10 +412,7 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-  // Reference max of the scaled scores (log2 domain): a finite stand-in for
-  // -inf, so that a stage whose keys are all masked for a row leaves it at
-  // p = 0 rather than producing 0 * inf.
-  float m_ref = -1e30f;
+  float m_ref = kNoMax;      // reference max of the scaled scores
   float l_run = 0.f;         // this lane's partial row sum
 
   const uint32_t k_lane = swz256(k_part + r32, g), v_lane = K_TILE + k_part * 256 + tr_base(lane);
@@ -523,7 +528,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-  float m_ref = -1e30f, l_run = 0.f;
+  float m_ref = kNoMax, l_run = 0.f;
   const int lim = min(tok + delta, Lk - 1), lim_w = delta;      // of token 0
   const uint32_t k_lane = swz256(r32, g), v_lane = kFewTile + tr_base(lane);
   // The queries are here before the walk (the compiler waits for them and, with them, for

@@ -2,6 +2,7 @@
 definition in 64 bits (bounds in varlen_ref.py), and what the calls refuse."""
 
 import ctypes
+import random
 
 import pytest
 import torch
@@ -31,6 +32,8 @@ CASES = [  # query lengths, key lengths (None: the same), Hq, Hkv, causal
     ([5], [3], 4, 2, True),                         # rows that see nothing
     ([0, 7, 0, 0, 130, 1, 0], None, 4, 1, True),
     ([3, 0, 64], [0, 5, 0], 6, 2, True),            # no keys, no queries
+    ([9], [0], 2, 1, True),                         # no keys at all
+    ([0, 0], [3, 140], 4, 2, False),                # no queries at all
     ([31, 32, 33, 127, 128, 129, 255, 256, 257], None, 8, 2, True),
     ([31, 32, 33, 127, 128, 129, 255, 256, 257], None, 6, 2, False),
     ([700, 1, 411, 128, 257, 551], None, 4, 1, True),
@@ -145,6 +148,58 @@ def test_extreme_scores():
     plan = upipe.VarlenPlan([0, n], Hq=2, Hkv=1, device=DEV)
     o, lse = upipe.attn_fwd_varlen(q, k, v, plan)
     R.check_forward(o, lse, R.Packed(q, k, v, [0, n], [0, n], True))
+
+
+@pytest.mark.gpu
+def test_scores_far_below_nought():
+    """Every score of a row about -1e36: the weights are what they are between equals."""
+    n = 130
+    q = torch.full((n, 1, D), 1e17, dtype=torch.bfloat16, device=DEV)
+    k = torch.full((n, 1, D), -1e18, dtype=torch.bfloat16, device=DEV)
+    v = _normal((n, 1, D), 3)
+    plan = upipe.VarlenPlan([0, n], Hq=1, Hkv=1, device=DEV)
+    o, lse = upipe.attn_fwd_varlen(q, k, v, plan)
+    mean = v.double().cumsum(0) / torch.arange(1, n + 1, device=DEV)[:, None, None]
+    size = v.double().abs().cumsum(0) / torch.arange(1, n + 1, device=DEV)[:, None, None]
+    # equal scores: equal weights, each rounded by half a step of bf16, as is the result
+    R.check("o", o, mean, R.BF16 * mean.abs() + 2 * R.BF16 * size)
+    score = float((q[0, 0].double() * k[0, 0].double()).sum()) / D ** 0.5
+    R.check("lse", lse, torch.full_like(lse, score, dtype=torch.float64),
+            torch.full_like(lse, (D + 8) * R.FP32 * abs(score), dtype=torch.float64))
+
+
+@pytest.mark.gpu
+def test_plan_on_another_device_is_refused():
+    q = _normal((4, 1, D), 1)
+    with pytest.raises(ValueError, match="devices"):
+        upipe.attn_fwd_varlen(q, q, q, upipe.VarlenPlan([0, 4], Hq=1, Hkv=1, device="cpu"))
+
+
+def _random_case(seed):
+    r = random.Random(seed)
+    n = r.choice([1, 2, 5, 17])
+    q = [r.choice([0, 1, 2, 31, 64, 127, 129, 300, 900]) for _ in range(n)]
+    k = [max(0, x + r.choice([0, 0, 0, 5, 400, 2000, -3, -x])) for x in q]
+    Hkv = r.choice([1, 2, 3, 8])
+    G = r.choice([1, 2, 3, 4, 5, 7, 8, 16, 21])
+    return q, k, min(Hkv, 64 // G) * G, min(Hkv, 64 // G), r.random() < 0.75
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("seed", range(8))
+def test_random_lengths_and_heads(seed):
+    lq, lk, Hq, Hkv, causal = _random_case(seed)
+    cu_q, cu_k = _cu(lq), _cu(lk)
+    print(f"random {lq} {lk} {Hq}/{Hkv} causal={causal}", flush=True)
+    q, dout = _normal((cu_q[-1], Hq, D), seed), _normal((cu_q[-1], Hq, D), seed + 50)
+    k, v = _normal((cu_k[-1], Hkv, D), seed + 100), _normal((cu_k[-1], Hkv, D), seed + 150)
+    plan = upipe.VarlenPlan(cu_q, cu_k, Hq=Hq, Hkv=Hkv, causal=causal, device=DEV)
+    o, lse = upipe.attn_fwd_varlen(q, k, v, plan)
+    grads = upipe.attn_bwd_varlen(q, k, v, o, lse, dout, plan)
+    torch.cuda.synchronize()
+    ref = R.Packed(q, k, v, cu_q, cu_k, causal, dout)
+    R.check_forward(o, lse, ref)
+    R.check_backward(*grads, ref)
 
 
 @pytest.mark.gpu
