@@ -297,9 +297,10 @@ typedef struct {
  * counts to host memory (8-byte aligned, of upipe_varlen_plan_size bytes; 0: invalid
  * or unsupported lengths); the caller copies the bytes to the device (16-byte
  * aligned).  The calls below take both: `plan` is read on the host, during the
- * call only, `plan_dev` by the kernels.  A plan serves any number of calls, on any
- * stream, also at once; a captured call keeps the list of work that it was captured
- * with.  Hkv | Hq <= 64, d = 128, up to 2^20 sequences of lengths up to 2^24 - 128.
+ * call only, `plan_dev` by the kernels, which it has to outlive.  A plan serves any
+ * number of calls, on any stream, also at once; a captured call keeps the list of work
+ * that it was captured with, and reads `plan_dev` at every replay.  Hkv | Hq <= 64, d = 128,
+ * up to 2^20 sequences of lengths up to 2^24 - 128.
  *
  *   q, o   rows [.., Hq, d], k, v rows [.., Hkv, d], up to the last offset at least;
  *          rows behind it are neither read nor written.  Rows of k and v are at
@@ -307,8 +308,8 @@ typedef struct {
  *   lse    fp32, head h of query row t at lse[h * lse_head + t]
  * Scores, softmax and sums are fp32; the weights are rounded to bf16 for their product
  * with v.  lse carries no rounding to bf16.  A masked value that is infinite or
- * not a number does not reach a row; a visible one does.  The results depend on the lengths
- * and head counts of the whole plan in their last bits.
+ * not a number does not reach a row; a visible one does.  The results depend on the
+ * lengths and head counts of the whole plan in their last bits.
  * ---------------------------------------------------------------------- */
 size_t upipe_varlen_plan_size(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int Hq, int Hkv,
                               int d, int causal);

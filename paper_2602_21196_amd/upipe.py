@@ -752,7 +752,9 @@ def _offsets(cu, name):
 class VarlenPlan:
     """The work of one batch of packed sequences: sequence s has the queries
     cu_q[s] .. cu_q[s+1] and the keys cu_k[s] .. cu_k[s+1] (the same, unless given).
-    Host offsets, 0 first.  Made once per batch, for all layers, forward and backward."""
+    Host offsets, 0 first.  Made once per batch, for all layers, forward and backward, on
+    any streams.  The kernels read its list on the device: keep the plan until the calls
+    that were given it have run, and with a captured graph of such calls."""
 
     def __init__(self, cu_q, cu_k=None, *, Hq, Hkv, causal=True, device="cuda"):
         torch = _torch()
@@ -818,7 +820,6 @@ def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     """(dq, dk, dv) of the packed q, k, v, with o and lse of attn_fwd_varlen and the
     same plan.  Rows behind the last sequence are left as they are in out = (dq, dk, dv),
     0 in new tensors."""
-    torch = _torch()
     Tq, Tk = plan.total_q, plan.total_k
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv), _packed(o, "o", Tq, plan.Hq))
