@@ -646,6 +646,22 @@ def _rows(t, name, shape=None):
     return upipe_heads(t.data_ptr(), stride[0] if T > 1 else H * head, head)
 
 
+def _dense(t, shape, dtype, name):
+    """Pointer of a dense GPU tensor of this shape (a tuple) and type."""
+    if not isinstance(t, _torch().Tensor) or t.shape != shape or t.dtype is not dtype:
+        _ptr(t, dtype, name)
+        _shape(t, shape, name)
+    if not (t.is_cuda and t.is_contiguous()):
+        _ptr(t, dtype, name)
+    return t.data_ptr()
+
+
+def _new_like(t):
+    """A dense tensor like t (new_empty(t.shape) takes half as long again)."""
+    torch = _torch()
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _call(fn, args, *tensors):
     """lib().fn(*args, stream) on the current stream of the tensors' device, made the
     current one; all of them (None: not given) have to be on it."""
@@ -684,20 +700,18 @@ def _norm_inputs(q, k, wq, wk, positions):
     vq = _rows(q, "q")
     T, Hq, d = q.shape
     vk = _rows(k, "k", (T, k.shape[1] if k.dim() == 3 else 1, d))
-    if wq.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"wq must be bfloat16 or float32, got {wq.dtype}")
-    _shape(wq, (d,), "wq")
-    _shape(wk, (d,), "wk")
-    _shape(positions, (T,), "positions")
+    w = wq.dtype
+    if w is not torch.bfloat16 and w is not torch.float32:
+        raise TypeError(f"wq must be bfloat16 or float32, got {w}")
     return (T, Hq, k.shape[1], vq, vk,
-            (_ptr(wq, wq.dtype, "wq"), _ptr(wk, wq.dtype, "wk"),
-             int(wq.dtype == torch.float32), _ptr(positions, torch.int64, "positions")))
+            (_dense(wq, (d,), w, "wq"), _dense(wk, (d,), w, "wk"), int(w is torch.float32),
+             _dense(positions, (T,), torch.int64, "positions")))
 
 
 def _pair_out(out, q, k, names):
     """The caller's two output tensors, like q and k, or two new dense ones."""
     if out is None:
-        return q.new_empty(q.shape), k.new_empty(k.shape)
+        return _new_like(q), _new_like(k)
     for t, like, n in zip(out, (q, k), names):
         _rows(t, n, like.shape)
     return tuple(out)
@@ -801,8 +815,8 @@ def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv))
     if out is None:
-        o = q.new_empty(q.shape)
-        lse = q.new_empty((plan.Hq, q.shape[0]), dtype=torch.float32)
+        o = _new_like(q)
+        lse = torch.empty(plan.Hq, q.shape[0], dtype=torch.float32, device=q.device)
         if Tq < q.shape[0]:
             o[Tq:] = 0
             lse[:, Tq:] = float("-inf")
@@ -824,7 +838,7 @@ def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv), _packed(o, "o", Tq, plan.Hq))
     if out is None:
-        out = tuple(t.new_empty(t.shape) for t in (q, k, v))
+        out = tuple(_new_like(t) for t in (q, k, v))
         for t, n in zip(out, (Tq, Tk, Tk)):
             if n < t.shape[0]:
                 t[n:] = 0
@@ -849,7 +863,8 @@ def _cache(t, name, B, Hkv):
     if not t.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
     cap = t.shape[1]
-    _shape(t, (B, cap, Hkv, 128), name)
+    if t.shape != (B, cap, Hkv, 128):
+        _shape(t, (B, cap, Hkv, 128), name)
     step, row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"{name} must have dense rows, got strides {t.stride()}")
@@ -864,7 +879,7 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
     torch = _torch()
     if q.dim() != 4:
         raise ValueError(f"q must be [B,nq,Hq,d], got {tuple(q.shape)}")
-    if k_cache.dim() != 4 or tuple(k_cache.shape) != tuple(v_cache.shape):
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
         raise ValueError("k_cache and v_cache must be [B,cap,Hkv,d], got "
                          f"{tuple(k_cache.shape)}, {tuple(v_cache.shape)}")
     if (k_prefix is None) != (v_prefix is None):
@@ -873,7 +888,8 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
     cap, Hkv = k_cache.shape[1:3]
     if B < 1 or cap < 1:
         raise ValueError(f"attn_decode: no sequences or no cache rows ({B}, {cap})")
-    _shape(lens, (B,), "lens")
+    if lens.shape != (B,):
+        _shape(lens, (B,), "lens")
     vq = _rows(_flat_tokens(q, "q"), "q")
     vk, k_step = _cache(k_cache, "k_cache", B, Hkv)
     vv, v_step = _cache(v_cache, "v_cache", B, Hkv)
@@ -884,17 +900,16 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
         vkp = _rows(k_prefix, "k_prefix", (P, Hkv, d))
         vvp = _rows(v_prefix, "v_prefix", (P, Hkv, d))
     if out is None:
-        o = q.new_empty(q.shape)
-        lse = q.new_empty((B, Hq, nq), dtype=torch.float32)
+        o = _new_like(q)
+        lse = torch.empty(B, Hq, nq, dtype=torch.float32, device=q.device)
     else:
         o, lse = out
         _shape(o, q.shape, "o")
-        _shape(lse, (B, Hq, nq), "lse")
     need = upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d)
     ws = _workspace(ws, need, q.device, "upipe_attn_decode_workspace_size")
     _call("upipe_attn_decode",
-          (vq, vk, k_step, vv, v_step, _ptr(lens, torch.int32, "lens"), vkp, vvp,
-           _rows(_flat_tokens(o, "o"), "o"), _ptr(lse, torch.float32, "lse"), B, nq, cap, P, Hq,
+          (vq, vk, k_step, vv, v_step, _dense(lens, (B,), torch.int32, "lens"), vkp,
+           vvp, _rows(_flat_tokens(o, "o"), "o"), _dense(lse, (B, Hq, nq), torch.float32, "lse"), B, nq, cap, P, Hq,
            Hkv, d, ws.data_ptr(), ws.numel()),
           q, k_cache, v_cache, lens, k_prefix, v_prefix, o, lse, ws)
     return o, lse
