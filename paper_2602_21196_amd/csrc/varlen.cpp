@@ -605,50 +605,77 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
     return UPIPE_ERR_INVALID_ARG;
   if (d != HEAD_DIM || Hq > kMaxHeads || cap > kMaxSeq || P > kMaxSeq || nq > 128 || B > 65536)
     return UPIPE_ERR_UNSUPPORTED;
-  // a row's sixteen lanes, or workgroups of 64 packed rows, a few parts each
-  return grid_fits(B * nq * Hq, 512) ? UPIPE_OK : UPIPE_ERR_UNSUPPORTED;
+  // A row's sixteen lanes, or workgroups of 64 packed rows, a few parts each; behind a
+  // prefix the workgroups of both.
+  const int64_t rows = B * nq * Hq;
+  return grid_fits(P > 0 ? 2 * rows + 8192 : rows, 512) ? UPIPE_OK : UPIPE_ERR_UNSUPPORTED;
+}
+
+// Parts of at least `least` of the stages for n workgroups, expected to end first: rounds of
+// the chip, each of the fixed us of a workgroup and those of its stages, and the merge's
+// us of a part.
+int best_parts(int64_t n, int64_t stages, int64_t least, double fixed, double stage, double merge,
+               double* est) {
+  int best = 1;
+  for (int64_t p = 1; p <= std::max<int64_t>(1, std::min<int64_t>(stages / least, 2 * kCUs)); ++p) {
+    const double t = (n * p + kCUs - 1) / kCUs * (fixed + (stages + p - 1) / p * stage) +
+                     merge * n * p;
+    if (p == 1 || t < *est) {
+      best = (int)p;
+      *est = t;
+    }
+  }
+  return best;
 }
 
 // The prefix's workgroups: 256, 128 or 64 packed rows (1, 2 or 4 key parts inside)
-// against one of `parts` parts of it, expected to end first.  us of a stage and of a
+// against one of some parts of it.  us of a stage and of a
 // workgroup besides (its rows of 16384 x 8 heads, 64 a sequence, 1 | 2 | 4: 64 sequences
 // 42 | 42 | 47 us, 256 sequences 142 | 150 | 179, 64 of one head of 8 rows 20 | 18 | 15).
-constexpr double kPrefixStage[3] = {4.2, 2.25, 1.3}, kPrefixFixed = 8.0;
+constexpr double kPrefixStage[3] = {4.2, 2.25, 1.3}, kCacheFixed = 8.0;
+// us of a stage of 64 rows of a cache, and of 32 with the prefix beside them: 64 caches of 900
+// rows, 128 packed rows each, without a prefix in 1 | 2 | 4 parts 20 | 17 + 7 | 27 + 8 us, 4
+// of 15000, 256 rows x 4 heads, 2 | 4 | 16 110 | 66 | 99; with one, 8 rows: one of 131071
+// in 128 | 256 parts 20 | 24, 24 of 1 to 16384, 8 heads 2 | 4 | 16 131 | 116 | 131, 64 of
+// 1 to 1024, 8 heads, 1 | 2 81 | 88.
+constexpr double kCacheStage = 2.2, kFewStage = 2.0;
 
 void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
-  const int64_t stages = (P + 127) / 128;
   double best = 0.0;
   for (int i = 0; i < 3; ++i) {
     const int64_t n = (rows * kFwdParts[i] + 255) / 256 * Hkv;
-    for (int64_t parts = 1; parts <= std::min<int64_t>(stages, 2 * kCUs); ++parts) {
-      const int64_t rounds = (n * parts + kCUs - 1) / kCUs;
-      const double est = rounds * (kPrefixFixed + (stages + parts - 1) / parts * kPrefixStage[i]) +
-                         kMergePart * n * parts * (4.0 / kFwdParts[i]);
-      if (best == 0.0 || est < best) {
-        best = est;
-        p->prefix_ks = kFwdParts[i];
-        p->prefix_parts = (int)parts;
-      }
-      if (rounds > 4) break;
+    double est;
+    const int parts = best_parts(n, (P + 127) / 128, 1, kCacheFixed, kPrefixStage[i],
+                                 kMergePart * (4.0 / kFwdParts[i]), &est);
+    if (i == 0 || est < best) {
+      best = est;
+      p->prefix_ks = kFwdParts[i];
+      p->prefix_parts = parts;
     }
   }
 }
 
-// The lengths are on the device: the cut goes by the capacity, and a part is the
-// same share of whatever a cache holds.  About four workgroups a CU even out caches of
-// different lengths (24 of 1 to 16384 rows, 8 heads: 1 | 2 | 4 | 8 a CU 176 | 145 |
-// 110 | 110 us), of 512 rows at least (131072 rows of one cache, parts of 256 | 512 |
-// 1024: 48 | 37 | 33 us before the merge had its loads under way together, 23 with 512).
-// Up to 32 packed rows a cache goes by few_rows_kernel (64 caches of 512 rows, 8 heads of
-// 8 rows: 25 us, by the tiles of 64 rows 37; one of 131071 rows 16.5 and 17).
+// The lengths are on the device: the cut goes by the capacity, and a part is the same
+// share of whatever a cache holds.  Up to 32 packed rows a cache go by few_rows_kernel (64
+// caches of 512 rows, 8 heads of 8 rows: 25 us, by the tiles of 64 rows 37; one of 131071
+// rows 16.5 and 17).  Its parts without a prefix: about four workgroups a CU even out
+// caches of different lengths (24 of 1 to 16384 rows, 8 heads: 1 | 2 | 4 | 8 a CU 176 |
+// 145 | 110 | 110 us), of 512 rows at least (131072 rows of one cache, parts of 256 | 512
+// | 1024: 48 | 37 | 33 us before the merge had its loads under way together, 23 with 512).
 CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv) {
   CachePlan p;
   p.rows = B * nq * Hq;
-  const int64_t G = Hq / Hkv;
+  const int64_t G = Hq / Hkv, stages = (cap + 127) / 128;
   p.few = nq * G <= 32;
   const int64_t groups = B * Hkv * (p.few ? 1 : (nq * G + 63) / 64);
-  const int64_t least = (cap + 511) / 512;      // parts of 512 rows
-  p.splits = (int)std::max<int64_t>(1, std::min((4 * kCUs + groups - 1) / groups, least));
+  double est;
+  if (!p.few)
+    p.splits = best_parts(groups, stages, 4, kCacheFixed, kCacheStage, kMergePart, &est);
+  else if (P > 0)
+    p.splits = best_parts(groups, stages, 8, kCacheFixed, kFewStage, kMergePart, &est);
+  else
+    p.splits = (int)std::max<int64_t>(
+        1, std::min((4 * kCUs + groups - 1) / groups, (cap + 511) / 512));
   if (P > 0) plan_prefix(B * nq * G, P, Hkv, &p);
   return p;
 }
@@ -710,17 +737,7 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     a.part_lse = a.part_o + cache_parts(p) * p.rows * HEAD_DIM;
     a.Hkv = Hkv;
     a.G = G;
-    if (P > 0) {
-      a.k = view_of(k_prefix);
-      a.v = view_of(v_prefix);
-      a.one.Lq = (int32_t)T;
-      a.one.Lk = (int32_t)P;
-      a.one.parts = p.prefix_parts;
-      a.causal = 0;
-      const int64_t tiles = (T * G * p.prefix_ks + 255) / 256;
-      UPIPE_LAUNCH(kRowsFwd, stream,
-                   launch_rows_fwd(kRowsOne, p.prefix_ks, a, tiles * p.prefix_parts, stream));
-    }
+    RowFwdArgs one = a;
     a.k = view_of(k);
     a.v = view_of(v);
     a.k.batch = k_cache;
@@ -733,11 +750,21 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     a.splits = p.splits;
     a.part0 = p.prefix_parts;
     a.lse_head = nq;
-    if (p.few) {
-      UPIPE_LAUNCH(kRowsFwd, stream, launch_few_rows_fwd(a, B * p.splits, stream));
+    const int64_t blocks = (p.few ? 1 : ((int64_t)nq * G + 63) / 64) * B * p.splits;
+    if (P > 0) {
+      one.k = view_of(k_prefix);
+      one.v = view_of(v_prefix);
+      one.one.Lq = (int32_t)T;
+      one.one.Lk = (int32_t)P;
+      one.one.parts = p.prefix_parts;
+      const int64_t tiles = (T * G * p.prefix_ks + 255) / 256;
+      UPIPE_LAUNCH(kRowsFwd, stream,
+                   launch_rows_prefix(p.prefix_ks, p.few, one, a, tiles * p.prefix_parts, blocks,
+                                      stream));
+    } else if (p.few) {
+      UPIPE_LAUNCH(kRowsFwd, stream, launch_few_rows_fwd(a, blocks, stream));
     } else {
-      const int64_t tiles = ((int64_t)nq * G + 63) / 64;
-      UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, a, tiles * B * p.splits, stream));
+      UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, a, blocks, stream));
     }
     if (cache_parts(p) == 1) return UPIPE_OK;
     RowMergeArgs m{};

@@ -88,6 +88,10 @@ hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks
 // Caches with at most 32 packed rows (nq G) each: `blocks` as above, parts first.
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
 
+// The same caches behind a prefix (p), both in one launch.
+hipError_t launch_rows_prefix(int ks, bool few, const RowFwdArgs& p, const RowFwdArgs& c,
+                              int64_t prefix_blocks, int64_t cache_blocks, hipStream_t st);
+
 struct RowMergeArgs {
   const float *part_o, *part_lse;
   HeadView o;

@@ -306,23 +306,23 @@ __device__ __forceinline__ void write_row(const RowFwdArgs& a, bool part, const 
   if (g == 0) a.lse[lse_at + h * a.lse_head + tok] = row_lse;
 }
 
-// A workgroup: BQ packed rows of one key/value head against a range of its keys.
+// A workgroup: BQ packed rows of one key/value head against a range of its keys.  It is
+// number `block` of `blocks`, all heads'.
 template <int KS, int MODE>
-__global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
+__device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int block, int blocks) {
   constexpr int NQW = 8 / KS;            // waves along the rows
   constexpr int NT = 4 / KS;             // 32-key tiles of a stage per wave
   constexpr int BQ = 32 * NQW;           // rows per workgroup
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
   const int t = threadIdx.x;
   const int lane = t & 63;
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wq = KS == 1 ? w : w % NQW, ks = KS == 1 ? 0 : w / NQW;
   const int r32 = lane & 31, g = lane >> 5;
-  const int G = a.G, Hq = a.Hkv * G, items = gridDim.x / a.Hkv;
+  const int G = a.G, Hq = a.Hkv * G, items = blocks / a.Hkv;
   // A prefix's parts go round the XCDs, not its heads: an XCD that reads one head of
   // eight, 256 bytes out of every 2 KB, uses two of its L2's sixteen channels.
-  const int kvh = MODE == kRowsOne ? blockIdx.x / items : blockIdx.x % a.Hkv;
-  const int idx = MODE == kRowsOne ? blockIdx.x % items : blockIdx.x / a.Hkv;
+  const int kvh = MODE == kRowsOne ? block / items : block % a.Hkv;
+  const int idx = MODE == kRowsOne ? block % items : block / a.Hkv;
 
   RowItem it;
   int64_t cache = 0, lse_at, part_rows;
@@ -457,6 +457,12 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
   write_row(a, part, it, part_rows, lse_at, tok, kvh * G + hg, Hq, g, oacc, m_ref, l_tot);
 }
 
+template <int KS, int MODE>
+__global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  rows_fwd<KS, MODE>(a, smem, blockIdx.x, gridDim.x);
+}
+
 // Up to 32 packed rows of one cache and key/value head: a wave takes every NW-th 32-key
 // tile of the workgroup's part, each by itself: it copies its tile's K and V rows into
 // its own LDS, two tiles deep, waits for its own copies and meets the other waves only at
@@ -464,14 +470,14 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
 // hide behind the other's stream.
 constexpr int kFewWaves = 2;
 constexpr int kFewTile = 32 * HEAD_DIM * 2;        // K or V rows of a tile: 8 KB
-constexpr int kFewLds = kFewWaves * 4 * kFewTile;
 
-__global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs a) {
-  __shared__ __attribute__((aligned(1024))) char smem[kFewLds];
+template <int NW>
+__device__ __forceinline__ void few_rows(const RowFwdArgs& a, char* smem, int block) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r32 = lane & 31, g = lane >> 5;
-  const int kvh = blockIdx.x % a.Hkv, idx = blockIdx.x / a.Hkv, G = a.G, Hq = a.Hkv * G;
+  if (w >= NW) return;
+  const int kvh = block % a.Hkv, idx = block / a.Hkv, G = a.G, Hq = a.Hkv * G;
   const int b = idx / a.splits;
   RowItem it{};
   it.part = idx % a.splits;
@@ -511,7 +517,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
     }
   };
   copy(t0 + w, lds);
-  copy(t0 + w + kFewWaves, lds + 2 * kFewTile);
+  copy(t0 + w + NW, lds + 2 * kFewTile);
 
   bf16x8 qf[8];
 #pragma unroll
@@ -535,7 +541,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
   // the first copies): within it, it would wait for every copy.
 #pragma unroll
   for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
-  for (int t = t0 + w, n = 0; t < t1; t += kFewWaves, ++n) {
+  for (int t = t0 + w, n = 0; t < t1; t += NW, ++n) {
     const uint32_t boff = (w * 4 + 2 * (n & 1)) * kFewTile;
     // This tile's 16 copies have landed; the next one's may be under way.
     asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
@@ -543,7 +549,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
                  l_run, []() {}, []() {});
     // Every read of the tile is done: its place takes the copies of the next but one.
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    copy(t + 2 * kFewWaves, lds_address(smem) + boff);
+    copy(t + 2 * NW, lds_address(smem) + boff);
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the last, empty copies have ended
   float l_tot = l_run + __shfl_xor(l_run, 32);
@@ -567,7 +573,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
   __syncthreads();
   if (w > 0) return;
 #pragma unroll
-  for (int p = 0; p < kFewWaves - 1; ++p) {
+  for (int p = 0; p < NW - 1; ++p) {
     const float* part = fold + p * (4096 + 128);
     const float m_p = part[4096 + lane], l_p = part[4096 + 64 + lane];
     const float m_new = fmaxf(m_ref, m_p);
@@ -590,6 +596,27 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
   it.part += a.part0;
   write_row(a, a.splits + a.part0 > 1, it, (int64_t)a.B * a.nq * Hq, it.p0, tok, kvh * G + hg,
             Hq, g, oacc, m_ref, l_tot);
+}
+
+__global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[kFewWaves * 4 * kFewTile];
+  few_rows<kFewWaves>(a, smem, blockIdx.x);
+}
+
+// A shared prefix and the caches behind it in one launch, n_cache workgroups of the caches
+// first: they wait for memory, and the prefix's first ones start where they end.  Against
+// one launch each, without the merge, us: 64 caches of 1 to 1024 rows on 16384, 64 heads
+// on 8 80 | 86; 200 of 900 on 32768 359 | 415; 64 of 200 on 4096 41 | 41; 8 of 900 on
+// 2048, 8 heads on 1 12 | 23; the prefix first 86, 376, 41, 12, both by turns 92, 398,
+// 46, 12.
+template <int KS, bool FEW>
+__global__ __launch_bounds__(512, 1) void rows_prefix_kernel(RowFwdArgs p, RowFwdArgs c,
+                                                             int n_cache) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  const int b = blockIdx.x;
+  if (b >= n_cache) rows_fwd<KS, kRowsOne>(p, smem, b - n_cache, gridDim.x - n_cache);
+  else if (FEW) few_rows<4>(c, smem, b);
+  else rows_fwd<4, kRowsCache>(c, smem, b, n_cache);
 }
 
 // The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
@@ -718,10 +745,6 @@ hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks
     if (ks == 1) UPIPE_ROWS(1, kRowsPlanned);
     else if (ks == 2) UPIPE_ROWS(2, kRowsPlanned);
     else UPIPE_ROWS(4, kRowsPlanned);
-  } else if (mode == kRowsOne) {
-    if (ks == 1) UPIPE_ROWS(1, kRowsOne);
-    else if (ks == 2) UPIPE_ROWS(2, kRowsOne);
-    else UPIPE_ROWS(4, kRowsOne);
   } else {
     UPIPE_ROWS(4, kRowsCache);
   }
@@ -731,6 +754,25 @@ hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks
 
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
   hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)(blocks * a.Hkv)), dim3(64 * kFewWaves), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rows_prefix(int ks, bool few, const RowFwdArgs& p, const RowFwdArgs& c,
+                              int64_t prefix_blocks, int64_t cache_blocks, hipStream_t st) {
+  const int n_cache = (int)(cache_blocks * c.Hkv);
+  const dim3 grid((unsigned)(prefix_blocks * p.Hkv + n_cache));
+#define UPIPE_PREFIX(K, F) \
+  hipLaunchKernelGGL((rows_prefix_kernel<K, F>), grid, dim3(512), 0, st, p, c, n_cache)
+  if (few) {
+    if (ks == 1) UPIPE_PREFIX(1, true);
+    else if (ks == 2) UPIPE_PREFIX(2, true);
+    else UPIPE_PREFIX(4, true);
+  } else {
+    if (ks == 1) UPIPE_PREFIX(1, false);
+    else if (ks == 2) UPIPE_PREFIX(2, false);
+    else UPIPE_PREFIX(4, false);
+  }
+#undef UPIPE_PREFIX
   return hipGetLastError();
 }
 

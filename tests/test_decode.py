@@ -206,3 +206,31 @@ def test_binding_refuses():
         upipe.attn_decode(q, c, c, n[:1])
     with pytest.raises(ValueError, match="evenly"):
         upipe.attn_decode(torch.zeros((2, 3, 4, D), dtype=torch.bfloat16)[:, :2], c, c, n)
+
+
+# A prefix and caches in one launch: 1, 2 and 4 key parts of the prefix's rows, the caches by
+# tiles of 64 packed rows or as up to 32 of them.
+BEHIND = [  # B, lens up to, cap, nq, Hq, Hkv, P
+    (2, 300, 1000, 40, 8, 2, 700),
+    (3, 2000, 2048, 16, 16, 2, 3000),
+    (40, 60, 64, 8, 64, 8, 1000),
+    (64, 40, 48, 16, 64, 1, 300),
+    (96, 30, 32, 4, 64, 8, 600),
+    (256, 9, 16, 4, 64, 8, 260),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("i", range(len(BEHIND)))
+def test_many_tokens_behind_a_prefix(i):
+    B, most, cap, nq, Hq, Hkv, P = BEHIND[i]
+    print(f"{B} caches of up to {most}/{cap}, nq={nq} {Hq}/{Hkv} P={P}", flush=True)
+    lens = [most * (b * b % 7) // 6 for b in range(B)]
+    q, kv = _normal((B, nq, Hq, D), 90 * i), _normal((B, cap, 2, Hkv, D), 90 * i + 1)
+    k, v = kv[:, :, 0], kv[:, :, 1]
+    for b, n in enumerate(lens):
+        kv[b, n:] = float("nan")
+    kp, vp = _normal((P, Hkv, D), 90 * i + 2), _normal((P, Hkv, D), 90 * i + 3)
+    o, lse = upipe.attn_decode(q, k, v, torch.tensor(lens, dtype=torch.int32, device=DEV), kp, vp)
+    torch.cuda.synchronize()
+    _check(o, lse, _Ref(q, k, v, lens, kp, vp))
