@@ -10,8 +10,7 @@
 #include <string.h>
 
 #include <algorithm>
-#include <functional>
-#include <utility>
+#include <cmath>
 #include <vector>
 
 #include "../../include/upipe.h"
@@ -33,24 +32,55 @@ constexpr int64_t kMaxRowStride = int64_t(1) << 22;
 bool grid_fits(int64_t blocks, int threads) { return blocks < (int64_t(1) << 32) / threads; }
 constexpr int kCUs = 256;
 
+// Calls f(i) for the items in the order of their keys (>= 0), the largest first, of one key
+// in the order they came.
+template <class F>
+void descending(const std::vector<int>& keys, F&& f) {
+  int most = 0;
+  for (int k : keys) most = std::max(most, k);
+  std::vector<int> order(keys.size());
+  if ((size_t)most < 4 * keys.size() + 1024) {      // counted: an eighth of the sort's time
+    std::vector<int> at(most + 2);
+    for (int k : keys) ++at[most - k + 1];
+    for (int k = 0; k < most; ++k) at[k + 1] += at[k];
+    for (size_t i = 0; i < keys.size(); ++i) order[at[most - keys[i]]++] = (int)i;
+  } else {
+    for (size_t i = 0; i < keys.size(); ++i) order[i] = (int)i;
+    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return keys[a] > keys[b]; });
+  }
+  for (int i : order) f(i);
+}
+
 // Time at which the last of these workgroups ends, `copies` of each: longest first,
-// each to the first of the CUs that is free, one to a CU, taking fixed + units * unit.
-double makespan(std::vector<int>* units, int copies, double fixed, double unit) {
-  std::sort(units->begin(), units->end(), std::greater<int>());
+// each to the first of the CUs that is free, one to a CU, taking fixed + units * unit.  Where
+// even an even spread would end after `limit` that is enough: infinity.
+double makespan(const std::vector<int>& units, int copies, double fixed, double unit,
+                double limit) {
+  double all = 0.0, longest = 0.0;
+  for (int u : units) {
+    all += fixed + u * unit;
+    longest = std::max(longest, fixed + u * unit);
+  }
+  if (std::max(all * copies / kCUs, longest) >= limit) return INFINITY;
+  // The copies of a workgroup go to CUs that are free together: one of them counts.
+  const int cus = kCUs % copies == 0 ? kCUs / copies : kCUs;
+  if (cus < kCUs) copies = 1;
   float free[kCUs] = {};           // a heap, the first free one on top
   float end = 0.f;
-  for (int u : *units)
+  descending(units, [&](int n) {
+    const float time = (float)(fixed + units[n] * unit);
     for (int i = 0; i < copies; ++i) {
-      const float t = free[0] + (float)(fixed + u * unit);
+      const float t = free[0] + time;
       end = std::max(end, t);
       int at = 0;
-      for (int c; (c = 2 * at + 1) < kCUs; at = c) {
-        if (c + 1 < kCUs && free[c + 1] < free[c]) ++c;
+      for (int c; (c = 2 * at + 1) < cus; at = c) {
+        if (c + 1 < cus && free[c + 1] < free[c]) ++c;
         if (free[c] >= t) break;
         free[at] = free[c];
       }
       free[at] = t;
     }
+  });
   return end;
 }
 
@@ -123,10 +153,12 @@ FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causa
       parts += np > 1;
       stages += st;
     });
-    c.est = makespan(&units, Hkv, kFwdFixed, kFwdStage[i]);
-    if (parts > 0) c.est += kMergeFixed + kMergePart * parts * Hkv * (4.0 / c.ks);
+    const double merge =
+        parts > 0 ? kMergeFixed + kMergePart * parts * Hkv * (4.0 / c.ks) : 0.0;
     // parts take workspace: only for a gain
-    if (first || c.est < (parts > 0 ? 0.95 : 1.0) * best.est) best = c;
+    const double limit = first ? INFINITY : (parts > 0 ? 0.95 : 1.0) * best.est;
+    c.est = merge + makespan(units, Hkv, kFwdFixed, kFwdStage[i], limit - merge);
+    if (c.est < limit) best = c;
     first = false;
     return stages * Hkv;
   };
@@ -136,7 +168,8 @@ FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causa
     const int64_t stages = look(c, i), mean = (stages + kCUs - 1) / kCUs;      // of a CU
     // Near the whole chip's rate of the largest tiles: nothing to gain.
     if (i == 0 && best.est <= 1.1 * stages * kFwdStage[0] / kCUs) break;
-    if (units.empty() || units[0] <= 2 * mean) continue;       // no long ones to cut
+    // no long ones to cut
+    if (units.empty() || *std::max_element(units.begin(), units.end()) <= 2 * mean) continue;
     for (int64_t m : {mean, 2 * mean}) {
       c.most = (int)std::max<int64_t>(4, m);
       look(c, i);
@@ -161,7 +194,7 @@ void key_walk(const Lengths& s, int tpt, int kb, int causal, int* first, int* la
 }
 
 // Calls f(sequence, r0, key block, segment, segments, first tile, tiles) for every
-// workgroup of dK/dV.  The walks of a sequence's key blocks are prefixes of one list,
+// workgroup of dK/dV, those of a segment side by side.  The walks of a sequence's key blocks are prefixes of one list,
 // its tiles from the last one down.  That list is cut at every `most`-th tile, so that
 // the workgroups of a segment walk the same tiles side by side and share their lines
 // in L2 (walks cut each into even segments: 32768 rows of 8 heads on 1, 4330 | 4207 us).
@@ -170,12 +203,17 @@ void each_key(const std::vector<Lengths>& seqs, int G, int causal, int most, F&&
   const int tpt = tile_tokens(G);
   int64_t r0 = 0;
   for (size_t s = 0; s < seqs.size(); ++s) {
-    for (int kb = 0; kb < (seqs[s].Lk + 127) / 128; ++kb) {
-      int first, last;
-      key_walk(seqs[s], tpt, kb, causal, &first, &last);
-      const int n = last - first + 1, segs = n <= most ? 1 : (n + most - 1) / most;
-      for (int i = 0, done = 0; i < segs; ++i, done += most)
-        f((int)s, r0, kb, i, segs, last - done, segs > 1 ? std::min(n - done, most) : n);
+    const int kbs = (seqs[s].Lk + 127) / 128;
+    // Walks get shorter from key block to key block: `left` of them have a segment i.
+    for (int i = 0, left = kbs; left > 0; ++i) {
+      const int done = i > 0 ? i * most : 0;
+      for (int kb = 0; kb < left; ++kb) {
+        int first, last;
+        key_walk(seqs[s], tpt, kb, causal, &first, &last);
+        const int n = last - first + 1, segs = n <= most ? 1 : (n - 1) / most + 1;
+        if (i >= segs) left = kb;
+        else f((int)s, r0, kb, i, segs, last - done, segs > 1 ? std::min(n - done, most) : n);
+      }
     }
     r0 += (int64_t)((seqs[s].Lq + tpt - 1) / tpt) * 128;
   }
@@ -203,9 +241,10 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
       tiles += count;
     });
     if (n > 8 && slots * Hkv > kMaxSums) continue;
-    const double est = makespan(&units, Hkv, kKeyFixed, kKeyTile) +
-                       (slots > 0 ? kFoldFixed + kFoldSum * slots * Hkv : 0.0);
-    if (n == 8 || est < best_est) {
+    const double fold = slots > 0 ? kFoldFixed + kFoldSum * slots * Hkv : 0.0;
+    const double limit = n == 8 ? INFINITY : best_est;
+    const double est = fold + makespan(units, Hkv, kKeyFixed, kKeyTile, limit - fold);
+    if (est < limit) {
       best = most;
       best_est = est;
     }
@@ -243,8 +282,9 @@ int choose_dq(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
       units.push_back(st);
       stages += st;
     });
-    const double est = makespan(&units, Hkv, kDqFixed, kDqStage[i]);
-    if (i == 0 || est < best_est) {
+    const double limit = i == 0 ? INFINITY : best_est;
+    const double est = makespan(units, Hkv, kDqFixed, kDqStage[i], limit);
+    if (est < limit) {
       best = kFwdParts[i];
       best_est = est;
     }
@@ -255,10 +295,9 @@ int choose_dq(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
 
 // Longest first, in the order they came.
 template <class T>
-void longest_first(std::vector<std::pair<int, T>>* work, std::vector<T>* out) {
-  std::stable_sort(work->begin(), work->end(),
-                   [](const auto& a, const auto& b) { return a.first > b.first; });
-  for (const auto& w : *work) out->push_back(w.second);
+void longest_first(const std::vector<int>& units, const std::vector<T>& work, std::vector<T>* out) {
+  out->reserve(work.size());
+  descending(units, [&](int i) { out->push_back(work[i]); });
 }
 
 int check_lengths(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, int d, int causal,
@@ -330,35 +369,45 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
       p->merge.push_back({s.q0, h.part_rows, s.Lq, np, (int32_t)b, 0});
     h.part_rows += np * rows;
   }
-  std::vector<std::pair<int, RowItem>> fwd;
+  std::vector<int> units;
+  std::vector<RowItem> fwd;
   each_fwd(seqs, G, causal, c, [&](int i, int tile, int part, int np, int stages) {
     const Lengths& s = seqs[i];
-    fwd.push_back({stages, {s.q0, s.k0, p0[i], s.Lq, s.Lk, tile, part, np, 0}});
+    units.push_back(stages);
+    fwd.push_back({s.q0, s.k0, p0[i], s.Lq, s.Lk, tile, part, np, 0});
   });
-  longest_first(&fwd, &p->fwd);
+  longest_first(units, fwd, &p->fwd);
 
   const int tpt = tile_tokens(G);
   for (const Lengths& s : seqs) h.term_rows += (int64_t)((s.Lq + tpt - 1) / tpt) * 128;
-  std::vector<std::pair<int, KeyItem>> keys;
+  units.clear();
+  std::vector<KeyItem> keys;
+  std::vector<int32_t> slot0;      // of the sequence's key blocks
   each_key(seqs, G, causal, choose_segment(seqs, G, Hkv, causal),
            [&](int i, int64_t r0, int kb, int seg, int segs, int first, int count) {
              const Lengths& s = seqs[i];
-             if (seg == 0 && segs > 1) p->folds.push_back({s.k0, s.Lk, kb, (int32_t)h.slots, segs});
-             const int32_t slot = segs > 1 ? (int32_t)h.slots++ : -1;
-             keys.push_back({count, {s.q0, s.k0, r0, s.Lq, s.Lk, kb, first, count, slot}});
+             if (seg == 0) {
+               if (kb == 0) slot0.clear();
+               slot0.push_back((int32_t)h.slots);
+               if (segs > 1) {
+                 p->folds.push_back({s.k0, s.Lk, kb, (int32_t)h.slots, segs});
+                 h.slots += segs;
+               }
+             }
+             units.push_back(count);
+             keys.push_back({s.q0, s.k0, r0, s.Lq, s.Lk, kb, first, count,
+                             segs > 1 ? slot0[kb] + seg : -1});
            });
-  // of one length, the workgroups of a segment side by side
-  std::stable_sort(keys.begin(), keys.end(), [](const auto& a, const auto& b) {
-    return a.second.r0 != b.second.r0 ? a.second.r0 < b.second.r0 : a.second.first > b.second.first;
-  });
-  longest_first(&keys, &p->keys);
+  longest_first(units, keys, &p->keys);
   h.dq_ks = choose_dq(seqs, G, Hkv, causal);
-  std::vector<std::pair<int, TileItem>> dqs;
+  units.clear();
+  std::vector<TileItem> dqs;
   each_dq(seqs, G, causal, h.dq_ks, [&](int i, int64_t r0, int tile, int stages) {
     const Lengths& s = seqs[i];
-    dqs.push_back({stages, {s.q0, s.k0, r0, s.Lq, s.Lk, tile, 0}});
+    units.push_back(stages);
+    dqs.push_back({s.q0, s.k0, r0, s.Lq, s.Lk, tile, 0});
   });
-  longest_first(&dqs, &p->dqs);
+  longest_first(units, dqs, &p->dqs);
 
   auto fits = [&](size_t items, int threads) { return grid_fits((int64_t)items * Hkv, threads); };
   if (!fits(p->fwd.size(), 512) || !fits(p->merge.size(), 256) ||
