@@ -15,8 +15,10 @@
 // tensor's 16 weights (and its 16 sums of dw).  The angles are formed once per token and
 // pair of heads, in fp64 turns (positions to 2^32) with the frequencies from the
 // kernel's arguments.  The norm's sums, r, the rotation and the sums of dw are fp32; y,
-// dx and a bf16 dw are rounded once.  65536 tokens: 40 heads forward 258 us (5.2 TB/s, a
-// large copy 5.1), 72 heads backward 712 us (5.1 TB/s; a head at a time 742).
+// dx and a bf16 dw are rounded once.  65536 tokens: 40 heads forward 252 us (5.3 TB/s, a
+// large copy 5.1), 72 heads backward 708 us (5.1 TB/s; a head at a time 742); 4000 tokens, 40
+// heads 17 and 27 us (before the weights came by wide loads and without 64-bit divisions
+// 22 and 31).
 #include "common.h"
 #include "kernels.h"
 
@@ -40,30 +42,35 @@ __device__ __forceinline__ Row16 load_row(const bf16* p) {
   return {*reinterpret_cast<const bf16x8*>(p), *reinterpret_cast<const bf16x8*>(p + 64)};
 }
 
-__device__ __forceinline__ void load_weights(const void* w, int w_fp32, int j, float (&out)[16]) {
+// This lane's 16 weights.
+template <bool W32>
+__device__ __forceinline__ void load_weights(const void* w, int j, float (&out)[16]) {
+  if (W32) {
+    const f32x4* p = static_cast<const f32x4*>(w) + 2 * j;
+    const f32x4 v[4] = {p[0], p[1], p[16], p[17]};
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int at = 8 * j + (e & 7) + 64 * (e >> 3);
-    out[e] = w_fp32 ? static_cast<const float*>(w)[at]
-                    : (float)static_cast<const bf16*>(w)[at];
+    for (int e = 0; e < 16; ++e) out[e] = v[e >> 2][e & 3];
+  } else {
+    const Row16 v = load_row(static_cast<const bf16*>(w) + 8 * j);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      out[e] = (float)v.lo[e];
+      out[8 + e] = (float)v.hi[e];
+    }
   }
 }
 
 // The pairs of heads of one tensor that this lane group takes: pair first, first +
-// step, ..., as (token, first head of the pair) without a division in the loop.
+// step, ... (both in 32 bits), as token t < T and pair p of it.
 struct PairWalk {
-  int64_t t, left;
-  int p, pairs;
-  int64_t t_step;
-  int p_step;
-  __device__ __forceinline__ PairWalk(int64_t first, int64_t step, int64_t T, int H) {
+  int64_t t;
+  int p, pairs, t_step, p_step;
+  __device__ __forceinline__ PairWalk(uint32_t first, uint32_t step, int H) {
     pairs = (H + 1) / 2;
-    const int64_t n = T * pairs;
-    t = first / pairs;
-    p = (int)(first - t * pairs);
-    t_step = step / pairs;
-    p_step = (int)(step - t_step * pairs);
-    left = first < n ? (n - first + step - 1) / step : 0;
+    t = first / (uint32_t)pairs;
+    p = first - (uint32_t)t * pairs;
+    t_step = step / (uint32_t)pairs;
+    p_step = step - t_step * pairs;
   }
   __device__ __forceinline__ void next() {
     t += t_step;
@@ -72,7 +79,6 @@ struct PairWalk {
       p -= pairs;
       ++t;
     }
-    --left;
   }
 };
 
@@ -95,28 +101,42 @@ __device__ __forceinline__ const NormRopeSide& side_of(const NormRopeArgs& a, in
   return is_q ? a.q : a.k;
 }
 
+template <bool W32>
 __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
   int block, blocks;
   const NormRopeSide& s = side_of(a, block, blocks);
   const int j = threadIdx.x & 7;
-  PairWalk it((int64_t)block * kPairsPerBlock + (threadIdx.x >> 3),
-              (int64_t)blocks * kPairsPerBlock, a.T, s.H);
-  if (it.left <= 0) return;
+  PairWalk it(block * kPairsPerBlock + (threadIdx.x >> 3), blocks * kPairsPerBlock, s.H);
+  if (it.t >= a.T) return;
+  const bf16* x0 = s.x.p + 8 * j;
+  bf16* y0 = s.y.p + 8 * j;
+  // The rows of the walk's pair (an odd last head twice), past its end those of the last
+  // token, which go unused; a pair ahead (16000 tokens, 40 heads 62 -> 60.5 us; the
+  // backward's registers do not hold it: 708 -> 727).
+  auto load = [&](Row16 (&x)[2], int64_t& pos) {
+    const int64_t t = min(it.t, a.T - 1);
+    const bf16* xp = x0 + t * s.x.row;
+    x[0] = load_row(xp + 2 * it.p * s.x.head);
+    x[1] = load_row(xp + min(2 * it.p + 1, s.H - 1) * s.x.head);
+    pos = a.positions[t];
+  };
+  Row16 next[2];
+  int64_t next_pos;
+  load(next, next_pos);
   float w[16];
-  load_weights(s.w, a.w_fp32, j, w);
+  load_weights<W32>(s.w, j, w);
   double f[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = a.freq.turns[8 * j + e];
-  const bf16* x0 = s.x.p + 8 * j;
-  bf16* y0 = s.y.p + 8 * j;
-  for (; it.left > 0; it.next()) {
+  while (it.t < a.T) {
+    const int64_t t = it.t;
     const int h = 2 * it.p, n = min(2, s.H - h);
-    const bf16* xp = x0 + it.t * s.x.row + h * s.x.head;
-    Row16 x[2];
-    x[0] = load_row(xp);
-    if (n > 1) x[1] = load_row(xp + s.x.head);
+    const Row16 x[2] = {next[0], next[1]};
+    const double pos = (double)next_pos;
+    it.next();
+    load(next, next_pos);
     float c[8], sn[8];
-    angles((double)a.positions[it.t], f, c, sn);
+    angles(pos, f, c, sn);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if (u >= n) break;
@@ -137,7 +157,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
         y.lo[e] = (bf16)p;
         y.hi[e] = (bf16)q;
       }
-      bf16* yp = y0 + it.t * s.y.row + (h + u) * s.y.head;
+      bf16* yp = y0 + t * s.y.row + (h + u) * s.y.head;
       *reinterpret_cast<bf16x8*>(yp) = y.lo;
       *reinterpret_cast<bf16x8*>(yp + 64) = y.hi;
     }
@@ -145,25 +165,25 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a) {
 }
 
 // dx of every row, and each workgroup's sums of dw to partial[block][128].
+template <bool W32>
 __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormRopeArgs a,
                                                             float* __restrict__ partial) {
   __shared__ float sums[4][HEAD_DIM];
   int block, blocks;
   const NormRopeSide& s = side_of(a, block, blocks);
   const int j = threadIdx.x & 7;
-  PairWalk it((int64_t)block * kPairsPerBlock + (threadIdx.x >> 3),
-              (int64_t)blocks * kPairsPerBlock, a.T, s.H);
+  PairWalk it(block * kPairsPerBlock + (threadIdx.x >> 3), blocks * kPairsPerBlock, s.H);
+  const bf16* x0 = s.x.p + 8 * j;
+  const bf16* d0 = s.dy.p + 8 * j;
+  bf16* y0 = s.y.p + 8 * j;
   float w[16], dw[16];
-  load_weights(s.w, a.w_fp32, j, w);
+  load_weights<W32>(s.w, j, w);
   double f[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) f[e] = a.freq.turns[8 * j + e];
 #pragma unroll
   for (int e = 0; e < 16; ++e) dw[e] = 0.f;
-  const bf16* x0 = s.x.p + 8 * j;
-  const bf16* d0 = s.dy.p + 8 * j;
-  bf16* y0 = s.y.p + 8 * j;
-  for (; it.left > 0; it.next()) {
+  for (; it.t < a.T; it.next()) {
     const int h = 2 * it.p, n = min(2, s.H - h);
     const bf16* xp = x0 + it.t * s.x.row + h * s.x.head;
     const bf16* dp = d0 + it.t * s.dy.row + h * s.dy.head;
@@ -274,7 +294,9 @@ constexpr int kNormFwdBlocks = 4096, kNormBwdBlocks = 1024;
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t st) {
   a.blocks_q = norm_blocks(a.T, a.q.H, kNormFwdBlocks);
   const int blocks_k = norm_blocks(a.T, a.k.H, kNormFwdBlocks);
-  hipLaunchKernelGGL(norm_rope_kernel, dim3((unsigned)(a.blocks_q + blocks_k)), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)(a.blocks_q + blocks_k));
+  if (a.w_fp32) hipLaunchKernelGGL(norm_rope_kernel<true>, grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL(norm_rope_kernel<false>, grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -285,8 +307,9 @@ int64_t norm_rope_bwd_partials(int64_t T, int Hq, int Hkv) {
 hipError_t launch_norm_rope_bwd(NormRopeArgs a, float* partial, hipStream_t st) {
   a.blocks_q = norm_blocks(a.T, a.q.H, kNormBwdBlocks);
   const int blocks_k = norm_blocks(a.T, a.k.H, kNormBwdBlocks);
-  hipLaunchKernelGGL(norm_rope_bwd_kernel, dim3((unsigned)(a.blocks_q + blocks_k)), dim3(256), 0,
-                     st, a, partial);
+  const dim3 grid((unsigned)(a.blocks_q + blocks_k));
+  if (a.w_fp32) hipLaunchKernelGGL(norm_rope_bwd_kernel<true>, grid, dim3(256), 0, st, a, partial);
+  else hipLaunchKernelGGL(norm_rope_bwd_kernel<false>, grid, dim3(256), 0, st, a, partial);
   return hipGetLastError();
 }
 
