@@ -704,13 +704,31 @@ void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
   }
 }
 
+// Parts for few_rows_kernel, two workgroups a CU: of 1024 rows, unless they are more than
+// four a CU, or of 2048, unless they are more than sixteen; or up to twice as many (512
+// rows each at least) where that fills the chip, or whole rounds of it, better.  us with the
+// merge: 24 caches of 8192 rows, 8 heads, in 5 | 6 | 8 parts 153 | 172 | 156, of 1 to 16384
+// in 4 | 6 | 8 | 12 122 | 119 | 116 | 119; 64 of 1 to 16384 in 2 | 4 | 8 | 16 172 | 148 |
+// 139 | 154, 8 in 4 | 8 | 16 | 32 62 | 40 | 32 | 38; 40 of 8000, 2 heads, in 4 | 6 | 8 |
+// 12 80 | 69 | 83 | 72; 8 of 131000, one head, in 32 | 64 | 128 | 256 107 | 105 | 108 |
+// 113; one of 131072, parts of 256 | 512 | 1024 rows 48 | 37 | 33 before the merge had its
+// loads under way together, 23 with 512.
+int few_parts(int64_t groups, int64_t cap) {
+  const int64_t slots = 2 * kCUs, most = std::min<int64_t>((cap + 511) / 512, kMostParts);
+  const int64_t least =
+      std::min(most, std::max({int64_t(1), std::min((cap + 1023) / 1024, 2 * slots / groups),
+                               std::min((cap + 2047) / 2048, 8 * slots / groups)}));
+  int64_t best = least;
+  auto rounds = [&](int64_t p) { return (groups * p + slots - 1) / slots; };
+  for (int64_t p = least + 1; p <= std::min(most, std::max(2 * least, slots / groups)); ++p)
+    if (rounds(p) * best < rounds(best) * p) best = p;
+  return (int)best;
+}
+
 // The lengths are on the device: the cut goes by the capacity, and a part is the same
 // share of whatever a cache holds.  Up to 32 packed rows a cache go by few_rows_kernel (64
 // caches of 512 rows, 8 heads of 8 rows: 25 us, by the tiles of 64 rows 37; one of 131071
-// rows 16.5 and 17).  Its parts without a prefix: about four workgroups a CU even out
-// caches of different lengths (24 of 1 to 16384 rows, 8 heads: 1 | 2 | 4 | 8 a CU 176 |
-// 145 | 110 | 110 us), of 512 rows at least (131072 rows of one cache, parts of 256 | 512
-// | 1024: 48 | 37 | 33 us before the merge had its loads under way together, 23 with 512).
+// rows 16.5 and 17).
 CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv) {
   CachePlan p;
   p.rows = B * nq * Hq;
@@ -723,8 +741,7 @@ CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv)
   else if (P > 0)
     p.splits = best_parts(groups, stages, 8, kCacheFixed, kFewStage, kMergePart, &est);
   else
-    p.splits = (int)std::max<int64_t>(
-        1, std::min((4 * kCUs + groups - 1) / groups, (cap + 511) / 512));
+    p.splits = few_parts(groups, cap);
   if (P > 0) plan_prefix(B * nq * G, P, Hkv, &p);
   return p;
 }

@@ -234,3 +234,15 @@ def test_many_tokens_behind_a_prefix(i):
     o, lse = upipe.attn_decode(q, k, v, torch.tensor(lens, dtype=torch.int32, device=DEV), kp, vp)
     torch.cuda.synchronize()
     _check(o, lse, _Ref(q, k, v, lens, kp, vp))
+
+
+def test_no_more_parts_than_the_merge_holds():
+    """A row's parts, its cache's and the prefix's, have their weights in LDS: 2048 at most
+    (the workspace holds 129 words of every part's rows)."""
+    for cap in (1, 511, 513, 100000, 1 << 20, (1 << 24) - 128):
+        for P in (0, 1, 5000, (1 << 24) - 128):
+            for B, nq, Hq, Hkv in ((1, 1, 1, 1), (1, 1, 64, 8), (7, 3, 16, 2), (1, 128, 64, 1),
+                                   (300, 1, 64, 64), (3, 40, 8, 2), (65536, 1, 32, 8)):
+                size = upipe.upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, D)
+                parts, rest = divmod(size - 16, 129 * 4 * B * nq * Hq)
+                assert rest == 0 and 1 <= parts <= 2048, (cap, P, B, nq, Hq, Hkv, parts)
