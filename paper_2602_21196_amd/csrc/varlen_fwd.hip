@@ -12,11 +12,12 @@
 //     workgroup's waves: 256, 128 or 64 rows;
 //   - one launch over a host-made list of tiles, longest first;
 //   - a tile's keys cut into parts where tiles are few: fp32 results, merged.
-// Up to 32 packed rows a cache have a kernel of their own (few_rows_kernel).
+// Up to 32 packed rows a cache have a kernel of their own (few_rows_kernel); a prefix and the
+// caches behind it share a launch (rows_prefix_kernel).
 // What bounds it: MFMA issue where tiles fill the chip (131072 tokens, 4 heads on 1: 14.2
 // ms, 1240 TFLOP/s, as the forward over equal lengths; 65536 tokens in documents of up to
-// 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 110 us,
-// 4.6 TB/s; a plain read of as much 5.4), launches and one chain of stages in short calls.
+// 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 107 us,
+// 4.8 TB/s, 24 of 8192 5.4; a plain read of as much 5.4), launches and one chain of stages in short calls.
 #include "varlen.h"
 
 namespace upipe {
@@ -467,7 +468,8 @@ __global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
 // tile of the workgroup's part, each by itself: it copies its tile's K and V rows into
 // its own LDS, two tiles deep, waits for its own copies and meets the other waves only at
 // the end.  No barrier in the walk, and two workgroups a CU, so that one's start and end
-// hide behind the other's stream.
+// hide behind the other's stream.  Beside a prefix, whose workgroups have a CU each, four
+// waves of eight do the same.
 constexpr int kFewWaves = 2;
 constexpr int kFewTile = 32 * HEAD_DIM * 2;        // K or V rows of a tile: 8 KB
 
