@@ -656,10 +656,13 @@ def _dense(t, shape, dtype, name):
     return t.data_ptr()
 
 
-def _new_like(t):
-    """A dense tensor like t (new_empty(t.shape) takes half as long again)."""
+def _new_rows(t):
+    """A dense tensor like t [T, H, d] (new_empty(t.shape) takes half as long again), and
+    its upipe_heads."""
     torch = _torch()
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+    new = torch.empty_like(t, memory_format=torch.contiguous_format)
+    H, d = t.shape[-2:]
+    return new, upipe_heads(new.data_ptr(), H * d, d)
 
 
 def _call(fn, args, *tensors):
@@ -709,12 +712,12 @@ def _norm_inputs(q, k, wq, wk, positions):
 
 
 def _pair_out(out, q, k, names):
-    """The caller's two output tensors, like q and k, or two new dense ones."""
+    """The caller's two output tensors, like q and k, or two new dense ones, each with its
+    upipe_heads."""
     if out is None:
-        return _new_like(q), _new_like(k)
-    for t, like, n in zip(out, (q, k), names):
-        _rows(t, n, like.shape)
-    return tuple(out)
+        return *_new_rows(q), *_new_rows(k)
+    a, b = out
+    return a, _rows(a, names[0], q.shape), b, _rows(b, names[1], k.shape)
 
 
 def qk_norm_rope(q, k, wq, wk, positions, base, eps=1e-6, out=None):
@@ -722,10 +725,9 @@ def qk_norm_rope(q, k, wq, wk, positions, base, eps=1e-6, out=None):
     elements, times wq / wk [d] (bf16 or fp32), rotated at positions [T] (int64).
     q, k and out = (q', k') may be strided views with dense rows; out may be (q, k)."""
     T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
-    yq, yk = _pair_out(out, q, k, ("q_out", "k_out"))
+    yq, vyq, yk, vyk = _pair_out(out, q, k, ("q_out", "k_out"))
     _call("upipe_qk_norm_rope",
-          (vq, vk, *rest, _rows(yq, "q_out"), _rows(yk, "k_out"), T, Hq, Hkv, q.shape[2],
-           float(base), float(eps)),
+          (vq, vk, *rest, vyq, vyk, T, Hq, Hkv, q.shape[2], float(base), float(eps)),
           q, k, wq, wk, positions, yq, yk)
     return yq, yk
 
@@ -735,15 +737,14 @@ def qk_norm_rope_bwd(q, k, wq, wk, positions, base, dq_out, dk_out, eps=1e-6, ou
     outputs.  out = (dq, dk) may be (dq_out, dk_out) or (q, k)."""
     torch = _torch()
     T, Hq, Hkv, vq, vk, rest = _norm_inputs(q, k, wq, wk, positions)
-    vdq, vdk = _rows(dq_out, "dq_out", q.shape), _rows(dk_out, "dk_out", k.shape)
-    dq, dk = _pair_out(out, q, k, ("dq", "dk"))
+    vdy = _rows(dq_out, "dq_out", q.shape), _rows(dk_out, "dk_out", k.shape)
+    dq, vdq, dk, vdk = _pair_out(out, q, k, ("dq", "dk"))
     dwq, dwk = torch.empty_like(wq), torch.empty_like(wk)
     ws = _workspace(ws, upipe_qk_norm_rope_bwd_workspace_size(T, Hq, Hkv, q.shape[2]), q.device,
                     "upipe_qk_norm_rope_bwd_workspace_size")
     _call("upipe_qk_norm_rope_bwd",
-          (vq, vk, *rest, vdq, vdk, _rows(dq, "dq"), _rows(dk, "dk"), dwq.data_ptr(),
-           dwk.data_ptr(), T, Hq, Hkv, q.shape[2], float(base), float(eps), ws.data_ptr(),
-           ws.numel()),
+          (vq, vk, *rest, *vdy, vdq, vdk, dwq.data_ptr(), dwk.data_ptr(), T, Hq, Hkv, q.shape[2],
+           float(base), float(eps), ws.data_ptr(), ws.numel()),
           q, k, wq, wk, positions, dq_out, dk_out, dq, dk, ws)
     return dq, dk, dwq, dwk
 
@@ -815,17 +816,18 @@ def attn_fwd_varlen(q, k, v, plan, out=None, ws=None):
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv))
     if out is None:
-        o = _new_like(q)
+        o, vo = _new_rows(q)
         lse = torch.empty(plan.Hq, q.shape[0], dtype=torch.float32, device=q.device)
         if Tq < q.shape[0]:
             o[Tq:] = 0
             lse[:, Tq:] = float("-inf")
     else:
         o, lse = out
+        vo = _packed(o, "o", Tq, plan.Hq)
     ws = _workspace(ws, plan.fwd_workspace, q.device, "upipe_attn_fwd_varlen_workspace_size")
     _call("upipe_attn_fwd_varlen",
-          (*views, _packed(o, "o", Tq, plan.Hq), *_packed_lse(lse, q, plan), plan.host,
-           plan.dev.data_ptr(), ws.data_ptr(), ws.numel()),
+          (*views, vo, *_packed_lse(lse, q, plan), plan.host, plan.dev.data_ptr(), ws.data_ptr(),
+           ws.numel()),
           q, k, v, o, lse, plan.dev, ws)
     return o, lse
 
@@ -838,13 +840,15 @@ def attn_bwd_varlen(q, k, v, o, lse, dout, plan, out=None, ws=None):
     views = (_packed(q, "q", Tq, plan.Hq), _packed(k, "k", Tk, plan.Hkv),
              _packed(v, "v", Tk, plan.Hkv), _packed(o, "o", Tq, plan.Hq))
     if out is None:
-        out = tuple(_new_like(t) for t in (q, k, v))
-        for t, n in zip(out, (Tq, Tk, Tk)):
+        (dq, vdq), (dk, vdk), (dv, vdv) = _new_rows(q), _new_rows(k), _new_rows(v)
+        for t, n in ((dq, Tq), (dk, Tk), (dv, Tk)):
             if n < t.shape[0]:
                 t[n:] = 0
-    dq, dk, dv = out
-    grads = (_packed(dout, "dout", Tq, plan.Hq), _packed(dq, "dq", Tq, plan.Hq),
-             _packed(dk, "dk", Tk, plan.Hkv), _packed(dv, "dv", Tk, plan.Hkv))
+    else:
+        dq, dk, dv = out
+        vdq, vdk, vdv = (_packed(dq, "dq", Tq, plan.Hq), _packed(dk, "dk", Tk, plan.Hkv),
+                         _packed(dv, "dv", Tk, plan.Hkv))
+    grads = (_packed(dout, "dout", Tq, plan.Hq), vdq, vdk, vdv)
     ws = _workspace(ws, plan.bwd_workspace, q.device, "upipe_attn_bwd_varlen_workspace_size")
     _call("upipe_attn_bwd_varlen",
           (*views, *_packed_lse(lse, q, plan), *grads, plan.host, plan.dev.data_ptr(),
@@ -900,16 +904,17 @@ def attn_decode(q, k_cache, v_cache, lens, k_prefix=None, v_prefix=None, out=Non
         vkp = _rows(k_prefix, "k_prefix", (P, Hkv, d))
         vvp = _rows(v_prefix, "v_prefix", (P, Hkv, d))
     if out is None:
-        o = _new_like(q)
+        o, vo = _new_rows(q)
         lse = torch.empty(B, Hq, nq, dtype=torch.float32, device=q.device)
     else:
         o, lse = out
         _shape(o, q.shape, "o")
+        vo = _rows(_flat_tokens(o, "o"), "o")
     need = upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, d)
     ws = _workspace(ws, need, q.device, "upipe_attn_decode_workspace_size")
     _call("upipe_attn_decode",
           (vq, vk, k_step, vv, v_step, _dense(lens, (B,), torch.int32, "lens"), vkp,
-           vvp, _rows(_flat_tokens(o, "o"), "o"), _dense(lse, (B, Hq, nq), torch.float32, "lse"), B, nq, cap, P, Hq,
+           vvp, vo, _dense(lse, (B, Hq, nq), torch.float32, "lse"), B, nq, cap, P, Hq,
            Hkv, d, ws.data_ptr(), ws.numel()),
           q, k_cache, v_cache, lens, k_prefix, v_prefix, o, lse, ws)
     return o, lse
