@@ -18,6 +18,19 @@ struct HeadView {
   int64_t row, head, batch;
 };
 
+// One launch, the arguments taken where they lie (kernel<<<>>> copies them first and
+// stores the launch's shape away in between: 3.3 us on the host with 768 bytes of them, 2.8 so).
+template <class T>
+struct AsIs {
+  using type = T;
+};
+template <class... P>
+hipError_t enqueue(void (*kernel)(P...), dim3 grid, int threads, hipStream_t st,
+                   const typename AsIs<P>::type&... args) {
+  void* at[] = {const_cast<void*>(static_cast<const void*>(&args))...};
+  return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, dim3(threads), at, 0, st);
+}
+
 // ---- layout (layout.hip) -------------------------------------------------
 // src [S, H, d] heads h0..h0+n-1  ->  dst [n, Sp, d]; rows >= S are zero.
 hipError_t launch_pack_rows(const bf16* src, int64_t S, int H, int h0, int n,

@@ -294,10 +294,8 @@ constexpr int kNormFwdBlocks = 4096, kNormBwdBlocks = 1024;
 hipError_t launch_norm_rope(NormRopeArgs a, hipStream_t st) {
   a.blocks_q = norm_blocks(a.T, a.q.H, kNormFwdBlocks);
   const int blocks_k = norm_blocks(a.T, a.k.H, kNormFwdBlocks);
-  const dim3 grid((unsigned)(a.blocks_q + blocks_k));
-  if (a.w_fp32) hipLaunchKernelGGL(norm_rope_kernel<true>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(norm_rope_kernel<false>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  return enqueue(a.w_fp32 ? norm_rope_kernel<true> : norm_rope_kernel<false>,
+                 dim3((unsigned)(a.blocks_q + blocks_k)), 256, st, a);
 }
 
 int64_t norm_rope_bwd_partials(int64_t T, int Hq, int Hkv) {
@@ -307,18 +305,15 @@ int64_t norm_rope_bwd_partials(int64_t T, int Hq, int Hkv) {
 hipError_t launch_norm_rope_bwd(NormRopeArgs a, float* partial, hipStream_t st) {
   a.blocks_q = norm_blocks(a.T, a.q.H, kNormBwdBlocks);
   const int blocks_k = norm_blocks(a.T, a.k.H, kNormBwdBlocks);
-  const dim3 grid((unsigned)(a.blocks_q + blocks_k));
-  if (a.w_fp32) hipLaunchKernelGGL(norm_rope_bwd_kernel<true>, grid, dim3(256), 0, st, a, partial);
-  else hipLaunchKernelGGL(norm_rope_bwd_kernel<false>, grid, dim3(256), 0, st, a, partial);
-  return hipGetLastError();
+  return enqueue(a.w_fp32 ? norm_rope_bwd_kernel<true> : norm_rope_bwd_kernel<false>,
+                 dim3((unsigned)(a.blocks_q + blocks_k)), 256, st, a, partial);
 }
 
 hipError_t launch_norm_dw_fold(const float* partial, int64_t T, int Hq, int Hkv, void* dwq,
                                void* dwk, int w_fp32, hipStream_t st) {
-  hipLaunchKernelGGL(norm_dw_fold_kernel, dim3(HEAD_DIM / 16, 2), dim3(1024), 0, st, partial,
-                     norm_blocks(T, Hq, kNormBwdBlocks), norm_blocks(T, Hkv, kNormBwdBlocks), dwq,
-                     dwk, w_fp32);
-  return hipGetLastError();
+  return enqueue(norm_dw_fold_kernel, dim3(HEAD_DIM / 16, 2), 1024, st, partial,
+                 norm_blocks(T, Hq, kNormBwdBlocks), norm_blocks(T, Hkv, kNormBwdBlocks), dwq, dwk,
+                 w_fp32);
 }
 
 }  // namespace upipe

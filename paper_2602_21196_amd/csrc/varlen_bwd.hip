@@ -492,26 +492,17 @@ __global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
 
 hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st) {
   auto inside = [&](const HeadView& v) { return v.row >= (a.G - 1) * v.head + HEAD_DIM; };
-  const dim3 grid((unsigned)(n * a.Hkv));
-  if (inside(a.q) && inside(a.dO))
-    hipLaunchKernelGGL(rows_dkdv_kernel<true>, grid, dim3(256), 0, st, a);
-  else
-    hipLaunchKernelGGL(rows_dkdv_kernel<false>, grid, dim3(256), 0, st, a);
-  return hipGetLastError();
+  return enqueue(inside(a.q) && inside(a.dO) ? rows_dkdv_kernel<true> : rows_dkdv_kernel<false>,
+                 dim3((unsigned)(n * a.Hkv)), 256, st, a);
 }
 
 hipError_t launch_rows_dkdv_fold(const RowBwdArgs& a, int64_t n, hipStream_t st) {
-  hipLaunchKernelGGL(rows_dkdv_fold_kernel, dim3((unsigned)(n * 16), (unsigned)a.Hkv), dim3(256), 0,
-                     st, a);
-  return hipGetLastError();
+  return enqueue(rows_dkdv_fold_kernel, dim3((unsigned)(n * 16), (unsigned)a.Hkv), 256, st, a);
 }
 
 hipError_t launch_rows_dq(int ks, const RowBwdArgs& a, int64_t n, hipStream_t st) {
-  const dim3 grid((unsigned)(n * a.Hkv));
-  if (ks == 1) hipLaunchKernelGGL(rows_dq_kernel<1>, grid, dim3(512), 0, st, a);
-  else if (ks == 2) hipLaunchKernelGGL(rows_dq_kernel<2>, grid, dim3(512), 0, st, a);
-  else hipLaunchKernelGGL(rows_dq_kernel<4>, grid, dim3(512), 0, st, a);
-  return hipGetLastError();
+  return enqueue(ks == 1 ? rows_dq_kernel<1> : ks == 2 ? rows_dq_kernel<2> : rows_dq_kernel<4>,
+                 dim3((unsigned)(n * a.Hkv)), 512, st, a);
 }
 
 }  // namespace upipe

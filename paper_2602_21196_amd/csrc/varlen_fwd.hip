@@ -741,56 +741,35 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
 }  // namespace
 
 hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
-  const dim3 grid((unsigned)(blocks * a.Hkv));
-#define UPIPE_ROWS(K, M) hipLaunchKernelGGL((rows_fwd_kernel<K, M>), grid, dim3(512), 0, st, a)
-  if (mode == kRowsPlanned) {
-    if (ks == 1) UPIPE_ROWS(1, kRowsPlanned);
-    else if (ks == 2) UPIPE_ROWS(2, kRowsPlanned);
-    else UPIPE_ROWS(4, kRowsPlanned);
-  } else {
-    UPIPE_ROWS(4, kRowsCache);
-  }
-#undef UPIPE_ROWS
-  return hipGetLastError();
+  return enqueue(mode == kRowsCache ? rows_fwd_kernel<4, kRowsCache>
+                 : ks == 1          ? rows_fwd_kernel<1, kRowsPlanned>
+                 : ks == 2          ? rows_fwd_kernel<2, kRowsPlanned>
+                                    : rows_fwd_kernel<4, kRowsPlanned>,
+                 dim3((unsigned)(blocks * a.Hkv)), 512, st, a);
 }
 
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
-  hipLaunchKernelGGL(few_rows_kernel, dim3((unsigned)(blocks * a.Hkv)), dim3(64 * kFewWaves), 0, st, a);
-  return hipGetLastError();
+  return enqueue(few_rows_kernel, dim3((unsigned)(blocks * a.Hkv)), 64 * kFewWaves, st, a);
 }
 
 hipError_t launch_rows_prefix(int ks, bool few, const RowFwdArgs& p, const RowFwdArgs& c,
                               int64_t prefix_blocks, int64_t cache_blocks, hipStream_t st) {
   const int n_cache = (int)(cache_blocks * c.Hkv);
-  const dim3 grid((unsigned)(prefix_blocks * p.Hkv + n_cache));
-#define UPIPE_PREFIX(K, F) \
-  hipLaunchKernelGGL((rows_prefix_kernel<K, F>), grid, dim3(512), 0, st, p, c, n_cache)
-  if (few) {
-    if (ks == 1) UPIPE_PREFIX(1, true);
-    else if (ks == 2) UPIPE_PREFIX(2, true);
-    else UPIPE_PREFIX(4, true);
-  } else {
-    if (ks == 1) UPIPE_PREFIX(1, false);
-    else if (ks == 2) UPIPE_PREFIX(2, false);
-    else UPIPE_PREFIX(4, false);
-  }
-#undef UPIPE_PREFIX
-  return hipGetLastError();
+  return enqueue(few ? (ks == 1   ? rows_prefix_kernel<1, true>
+                        : ks == 2 ? rows_prefix_kernel<2, true>
+                                  : rows_prefix_kernel<4, true>)
+                     : (ks == 1   ? rows_prefix_kernel<1, false>
+                        : ks == 2 ? rows_prefix_kernel<2, false>
+                                  : rows_prefix_kernel<4, false>),
+                 dim3((unsigned)(prefix_blocks * p.Hkv + n_cache)), 512, st, p, c, n_cache);
 }
 
 hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t items, hipStream_t st) {
-  const int64_t blocks = a.items != nullptr ? items : a.one_row ? a.rows : (a.rows + 15) / 16;
-#define UPIPE_MERGE(GP, P) \
-  hipLaunchKernelGGL((rows_merge_kernel<GP, P>), dim3((unsigned)blocks), dim3(256), 0, st, a)
-  if (a.items != nullptr) {
-    if (a.one_row) UPIPE_MERGE(16, true);
-    else UPIPE_MERGE(1, true);
-  } else {
-    if (a.one_row) UPIPE_MERGE(16, false);
-    else UPIPE_MERGE(1, false);
-  }
-#undef UPIPE_MERGE
-  return hipGetLastError();
+  const bool planned = a.items != nullptr;
+  const int64_t blocks = planned ? items : a.one_row ? a.rows : (a.rows + 15) / 16;
+  return enqueue(planned ? (a.one_row ? rows_merge_kernel<16, true> : rows_merge_kernel<1, true>)
+                         : (a.one_row ? rows_merge_kernel<16, false> : rows_merge_kernel<1, false>),
+                 dim3((unsigned)blocks), 256, st, a);
 }
 
 }  // namespace upipe
