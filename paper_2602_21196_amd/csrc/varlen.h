@@ -80,6 +80,7 @@ struct RowFwdArgs {
   RowItem one;               // a single sequence (the shared prefix)
   int Hkv, G, causal;
   int B, nq, splits, part0;  // caches: their first part among those of a row
+  bool ranked;               // caches: the longest first
 };
 enum RowMode { kRowsPlanned = 0, kRowsCache = 1, kRowsOne = 2 };
 // `blocks` items (of every key/value head).

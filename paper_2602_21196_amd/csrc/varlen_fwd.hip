@@ -307,6 +307,28 @@ __device__ __forceinline__ void write_row(const RowFwdArgs& a, bool part, const 
   if (g == 0) a.lse[lse_at + h * a.lse_head + tok] = row_lse;
 }
 
+// The n-th cache to be worked on and its valid rows: where a.ranked (up to 64 caches) the
+// longest first, since workgroups start in their order.  Lane i has cache i's length above
+// its place from the end, so that no two are alike; the n-th of these numbers bit by bit is
+// the largest that more than n of them reach (counting the larger ones of every lane
+// takes twice as long).
+__device__ __forceinline__ int nth_cache(const RowFwdArgs& a, int n, int& Lk) {
+  auto valid = [&](int i) { return (int)min(max((int64_t)a.lens[i], (int64_t)0), a.cap); };
+  if (!a.ranked) {
+    Lk = valid(n);
+    return n;
+  }
+  const int lane = threadIdx.x & 63;
+  const int len = lane < a.B ? valid(lane) : 0;
+  const uint32_t key = lane < a.B ? (uint32_t)len * 64 + (63 - lane) : 0;
+  uint32_t nth = 0;
+  for (uint32_t bit = 1u << (37 - __builtin_clz((uint32_t)a.cap)); bit != 0; bit >>= 1)
+    if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(key >= (nth | bit))) > n) nth |= bit;
+  const int b = __builtin_ctzll(__builtin_amdgcn_ballot_w64(lane < a.B && key == nth));
+  Lk = __builtin_amdgcn_readlane(len, b);
+  return b;
+}
+
 // A workgroup: BQ packed rows of one key/value head against a range of its keys.  It is
 // number `block` of `blocks`, all heads'.
 template <int KS, int MODE>
@@ -338,7 +360,8 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
     lse_at = 0;                  // always parts
     part_rows = (int64_t)it.Lq * Hq;
   } else {
-    const int tiles = (a.nq * G + BQ - 1) / BQ, b = idx / a.splits % a.B;
+    const int tiles = (a.nq * G + BQ - 1) / BQ;
+    const int b = nth_cache(a, idx / a.splits % a.B, it.Lk);
     it.tile = idx / a.splits / a.B % tiles;
     it.part = idx % a.splits + a.part0;
     it.parts = a.splits;
@@ -346,7 +369,6 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
     it.k0 = 0;
     it.p0 = it.q0 * Hq;
     it.Lq = a.nq;
-    it.Lk = (int)min(max((int64_t)a.lens[b], (int64_t)0), a.cap);
     cache = b;
     lse_at = it.q0 * Hq;
     part_rows = (int64_t)a.B * a.nq * Hq;
@@ -480,12 +502,12 @@ __device__ __forceinline__ void few_rows(const RowFwdArgs& a, char* smem, int bl
   const int r32 = lane & 31, g = lane >> 5;
   if (w >= NW) return;
   const int kvh = block % a.Hkv, idx = block / a.Hkv, G = a.G, Hq = a.Hkv * G;
-  const int b = idx / a.splits;
+  int Lk;
+  const int b = nth_cache(a, idx / a.splits, Lk);
   RowItem it{};
   it.part = idx % a.splits;
   it.q0 = (int64_t)b * a.nq;
   it.p0 = it.q0 * Hq;
-  const int Lk = (int)min(max((int64_t)a.lens[b], (int64_t)0), a.cap);
   const int n_rows = a.nq * G, delta = Lk - a.nq;
   const bool row_ok = r32 < n_rows;
   const int tok = r32 / G, hg = r32 - tok * G;

@@ -246,3 +246,23 @@ def test_no_more_parts_than_the_merge_holds():
                 size = upipe.upipe_attn_decode_workspace_size(B, nq, cap, P, Hq, Hkv, D)
                 parts, rest = divmod(size - 16, 129 * 4 * B * nq * Hq)
                 assert rest == 0 and 1 <= parts <= 2048, (cap, P, B, nq, Hq, Hkv, parts)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("nq,Hq,Hkv", [(1, 32, 8), (9, 20, 4)])
+def test_caches_of_very_different_lengths(nq, Hq, Hkv):
+    """More workgroups than start at once, caches alike and longest last among them: the
+    order in which they are worked on changes nothing else."""
+    lens, cap = [0, 3, 40, 40, 1, 2000, 700, 5, 40, 0, 9000, 16000, 333, 8192], 16000
+    B = len(lens)
+    q, kv = _normal((B, nq, Hq, D), 1), _normal((B, cap, 2, Hkv, D), 2)
+    k, v = kv[:, :, 0], kv[:, :, 1]
+    for b, n in enumerate(lens):
+        kv[b, n:] = float("nan")
+    ld = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    o, lse = upipe.attn_decode(q, k, v, ld)
+    turn = list(range(B))[::-1]
+    o2, lse2 = upipe.attn_decode(q[turn], k[turn], v[turn], ld[turn])
+    torch.cuda.synchronize()
+    _check(o, lse, _Ref(q, k, v, lens))
+    assert torch.equal(o2[turn], o) and torch.equal(lse2[turn], lse)
