@@ -52,20 +52,22 @@ void descending(const std::vector<int>& keys, F&& f) {
 }
 
 // Time at which the last of these workgroups ends, `copies` of each: longest first,
-// each to the first of the CUs that is free, one to a CU, taking fixed + units * unit.  Where
-// even an even spread would end after `limit` that is enough: infinity.
-double makespan(const std::vector<int>& units, int copies, double fixed, double unit,
+// each to the first place that is free, `per_cu` (1 or 2) of them a CU, taking fixed +
+// units * unit.  Where even an even spread would end after `limit` that is enough:
+// infinity.
+double makespan(const std::vector<int>& units, int copies, int per_cu, double fixed, double unit,
                 double limit) {
+  const int places = per_cu * kCUs;
   double all = 0.0, longest = 0.0;
   for (int u : units) {
     all += fixed + u * unit;
     longest = std::max(longest, fixed + u * unit);
   }
-  if (std::max(all * copies / kCUs, longest) >= limit) return INFINITY;
-  // The copies of a workgroup go to CUs that are free together: one of them counts.
-  const int cus = kCUs % copies == 0 ? kCUs / copies : kCUs;
-  if (cus < kCUs) copies = 1;
-  float free[kCUs] = {};           // a heap, the first free one on top
+  if (std::max(all * copies / places, longest) >= limit) return INFINITY;
+  // The copies of a workgroup go to places that are free together: one of them counts.
+  const int heap = places % copies == 0 ? places / copies : places;
+  if (heap < places) copies = 1;
+  float free[2 * kCUs] = {};       // the first free one on top
   float end = 0.f;
   descending(units, [&](int n) {
     const float time = (float)(fixed + units[n] * unit);
@@ -73,8 +75,8 @@ double makespan(const std::vector<int>& units, int copies, double fixed, double 
       const float t = free[0] + time;
       end = std::max(end, t);
       int at = 0;
-      for (int c; (c = 2 * at + 1) < cus; at = c) {
-        if (c + 1 < cus && free[c + 1] < free[c]) ++c;
+      for (int c; (c = 2 * at + 1) < heap; at = c) {
+        if (c + 1 < heap && free[c + 1] < free[c]) ++c;
         if (free[c] >= t) break;
         free[at] = free[c];
       }
@@ -89,31 +91,43 @@ struct Lengths {
   int32_t Lq, Lk;
 };
 
-// us of one 128-key stage of a forward workgroup with 1, 2, 4 key parts on a full
-// chip, and of a workgroup besides its stages.  What they lead to, us with 1 | 2 | 4 (the
-// chosen one first): 64 documents of 256 tokens, 4 heads, 1: 21 | 28 | 43; 8192 tokens, 8
-// heads on 2, 2: 142 | 181 (1) | 174 (4); 16384, 8 heads, 1: 477 | 519 | 636; 2048 in
-// documents of up to 700, 4 heads, 4: 16 | 27 (1) | 18 (2).
-constexpr double kFwdStage[3] = {3.5, 2.0, 1.2}, kFwdFixed = 3.0;
-constexpr int kFwdParts[3] = {1, 2, 4};
+// A workgroup of the forward or of dQ: eight waves over 256 rows, or over 128 or 64 with a
+// stage's keys in 2 or 4 parts, one a CU; or, half, four waves over 128 rows, two a CU, so
+// that one's loads and stores hide behind the other's products.  us of a stage, and besides
+// them of one alone and where they fill the chip and share its memory.
+struct Shape {
+  int ks;                // 256 / rows
+  bool half;
+  int keys, per_cu;      // of a stage
+  double stage, fixed, full;
+};
+// What they lead to, us with 1 | 2 | 4 | half (* the chosen one): 16 documents of 256 tokens,
+// 32 heads on 8, 52 | 51 | 71 | 36*; 100 of up to 700, 8 on 1, 87 | 109 | 166 | 73*; 8
+// of 2048, 8 on 1, 80* | 93 | 136 | 82; 8192 tokens, 4 on 1, 172 | 106 | 93* | 137; 32768
+// tokens, 4 on 1, 903* | 978 | 1182 | 1022; 512 tokens, 4 on 1, 22 | 16 | 14* | 17.
+constexpr Shape kFwdShapes[4] = {{1, false, 128, 1, 3.5, 3.0, 10.0},
+                                 {2, false, 128, 1, 2.0, 3.0, 7.0},
+                                 {4, false, 128, 1, 1.2, 3.0, 6.5},
+                                 {2, true, 64, 2, 1.9, 3.0, 6.5}};
 // us that a merge launch takes, and that it takes for one part of 64 rows.  16 queries of 8
 // heads on 50000 keys: in parts of 4 stages 18 + 5 us, of 16 26 + 5, whole 402; 500
 // queries on 16000 keys: parts of 8 stages 43 + 6, whole 134.
 constexpr double kMergeFixed = 4.0, kMergePart = 0.01;
 
 struct FwdChoice {
-  int ks = 1;
+  const Shape* shape = kFwdShapes;
   int most = 1 << 30;      // stages of a part
   double est = 0.0;
 };
 
 int row_tiles(int32_t Lq, int G, int rows) { return (int)(((int64_t)Lq * G + rows - 1) / rows); }
 
-// Stages of tile `tile` of `rows` packed rows.
-int tile_stages(const Lengths& s, int G, int rows, int tile, int causal) {
-  const int64_t last = (std::min<int64_t>((int64_t)(tile + 1) * rows, (int64_t)s.Lq * G) - 1) / G;
+// Stages of tile `tile` of a sequence's packed rows.
+int tile_stages(const Lengths& s, int G, const Shape& shape, int tile, int causal) {
+  const int64_t rows = 256 / shape.ks;
+  const int64_t last = (std::min((tile + 1) * rows, (int64_t)s.Lq * G) - 1) / G;
   const int64_t seen = causal ? std::min<int64_t>(s.Lk, last + 1 + s.Lk - s.Lq) : s.Lk;
-  return seen <= 0 ? 0 : (int)((seen + 127) / 128);
+  return seen <= 0 ? 0 : (int)((seen + shape.keys - 1) / shape.keys);
 }
 
 // Parts into which the keys of a sequence's tiles are cut so that none has more
@@ -126,26 +140,32 @@ int seq_parts(const Lengths& s, int most) {
 // Calls f(sequence, tile, part, parts, stages) for every workgroup of the forward.
 template <class F>
 void each_fwd(const std::vector<Lengths>& seqs, int G, int causal, const FwdChoice& c, F&& f) {
-  const int rows = 256 / c.ks;
   for (size_t i = 0; i < seqs.size(); ++i) {
     const Lengths& s = seqs[i];
     const int np = seq_parts(s, c.most);
-    for (int t = row_tiles(s.Lq, G, rows) - 1; t >= 0; --t) {
-      const int st = tile_stages(s, G, rows, t, causal), per = (st + np - 1) / np;
+    for (int t = row_tiles(s.Lq, G, 256 / c.shape->ks) - 1; t >= 0; --t) {
+      const int st = tile_stages(s, G, *c.shape, t, causal), per = (st + np - 1) / np;
       for (int p = 0; p < np; ++p)
         f((int)i, t, p, np, std::max(0, std::min(st, per * (p + 1)) - per * p));
     }
   }
 }
 
-// The split of waves (1, 2 or 4 parts of a stage's keys) and of keys over
-// workgroups whose list is expected to end first.
+// The time that a list of workgroups of a shape is expected to take.
+double shape_time(const std::vector<int>& units, int Hkv, const Shape& shape, double limit) {
+  const double share = std::min(1.0, (double)units.size() * Hkv / kCUs);
+  return makespan(units, Hkv, shape.per_cu, shape.fixed + share * (shape.full - shape.fixed),
+                  shape.stage, limit);
+}
+
+// The workgroups' shape, and the keys' split over them, whose list is expected to end
+// first.
 FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
   FwdChoice best;
   std::vector<int> units;
   bool first = true;
   // Stages of all workgroups.
-  auto look = [&](FwdChoice c, int i) {
+  auto look = [&](FwdChoice c) {
     units.clear();
     int64_t parts = 0, stages = 0;
     each_fwd(seqs, G, causal, c, [&](int, int, int, int np, int st) {
@@ -154,25 +174,26 @@ FwdChoice choose_fwd(const std::vector<Lengths>& seqs, int G, int Hkv, int causa
       stages += st;
     });
     const double merge =
-        parts > 0 ? kMergeFixed + kMergePart * parts * Hkv * (4.0 / c.ks) : 0.0;
+        parts > 0 ? kMergeFixed + kMergePart * parts * Hkv * (4.0 / c.shape->ks) : 0.0;
     // parts take workspace: only for a gain
     const double limit = first ? INFINITY : (parts > 0 ? 0.95 : 1.0) * best.est;
-    c.est = merge + makespan(units, Hkv, kFwdFixed, kFwdStage[i], limit - merge);
+    c.est = merge + shape_time(units, Hkv, *c.shape, limit - merge);
     if (c.est < limit) best = c;
     first = false;
     return stages * Hkv;
   };
-  for (int i = 0; i < 3; ++i) {
+  for (const Shape& shape : kFwdShapes) {
     FwdChoice c;
-    c.ks = kFwdParts[i];
-    const int64_t stages = look(c, i), mean = (stages + kCUs - 1) / kCUs;      // of a CU
+    c.shape = &shape;
+    const int64_t stages = look(c), mean = (stages + kCUs - 1) / kCUs;      // of a CU
     // Near the whole chip's rate of the largest tiles: nothing to gain.
-    if (i == 0 && best.est <= 1.1 * stages * kFwdStage[0] / kCUs) break;
+    if (shape.ks == 1 && best.est <= 1.1 * stages * shape.stage / kCUs) break;
     // no long ones to cut
-    if (units.empty() || *std::max_element(units.begin(), units.end()) <= 2 * mean) continue;
+    if (shape.half || units.empty()) continue;
+    if (*std::max_element(units.begin(), units.end()) <= 2 * mean) continue;
     for (int64_t m : {mean, 2 * mean}) {
       c.most = (int)std::max<int64_t>(4, m);
-      look(c, i);
+      look(c);
     }
   }
   return best;
@@ -194,7 +215,8 @@ void key_walk(const Lengths& s, int tpt, int kb, int causal, int* first, int* la
 }
 
 // Calls f(sequence, r0, key block, segment, segments, first tile, tiles) for every
-// workgroup of dK/dV, those of a segment side by side.  The walks of a sequence's key blocks are prefixes of one list,
+// workgroup of dK/dV, those of a segment side by side.  The walks of a sequence's key
+// blocks are prefixes of one list,
 // its tiles from the last one down.  That list is cut at every `most`-th tile, so that
 // the workgroups of a segment walk the same tiles side by side and share their lines
 // in L2 (walks cut each into even segments: 32768 rows of 8 heads on 1, 4330 | 4207 us).
@@ -243,7 +265,7 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
     if (n > 8 && slots * Hkv > kMaxSums) continue;
     const double fold = slots > 0 ? kFoldFixed + kFoldSum * slots * Hkv : 0.0;
     const double limit = n == 8 ? INFINITY : best_est;
-    const double est = fold + makespan(units, Hkv, kKeyFixed, kKeyTile, limit - fold);
+    const double est = fold + makespan(units, Hkv, 1, kKeyFixed, kKeyTile, limit - fold);
     if (est < limit) {
       best = most;
       best_est = est;
@@ -254,43 +276,45 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
   return best;
 }
 
-// us of a dQ stage with 1 (64 keys), 2 and 4 (128 keys) key parts on a full chip.  us with
-// 1 | 2 | 4: 64 documents of 256 tokens, 4 heads 26 | 37 | 56; 8192 tokens, 8 heads on 2
-// 262 | 198 | 223; 2048 in documents of up to 700, 4 heads 34 | 24 | 20.
-constexpr double kDqStage[3] = {2.5, 2.8, 1.6}, kDqFixed = 4.0;
+// Of dQ, as the forward's: 58* in halves against 76 (1) for 16 documents of 256 tokens, 109*
+// and 124 for 100 of up to 700, 116 and 111* for 8 of 2048; 8192 tokens, 4 heads on 1, 250 |
+// 144 | 114* | 184; 512 tokens 28 | 21 | 18* | 21.
+constexpr Shape kDqShapes[4] = {{1, false, 64, 1, 2.5, 4.0, 16.0},
+                                {2, false, 128, 1, 2.8, 4.0, 11.0},
+                                {4, false, 128, 1, 1.6, 4.0, 9.0},
+                                {2, true, 64, 2, 2.7, 4.0, 12.0}};
 
 // Calls f(sequence, r0, tile, stages) for every workgroup of dQ.
 template <class F>
-void each_dq(const std::vector<Lengths>& seqs, int G, int causal, int ks, F&& f) {
-  const int rows = 256 / ks, tpt = tile_tokens(G);
+void each_dq(const std::vector<Lengths>& seqs, int G, int causal, const Shape& shape, F&& f) {
+  const int tpt = tile_tokens(G);
   int64_t r0 = 0;
   for (size_t s = 0; s < seqs.size(); ++s) {
-    for (int t = row_tiles(seqs[s].Lq, G, rows) - 1; t >= 0; --t)
-      f((int)s, r0, t, tile_stages(seqs[s], G, rows, t, causal) * (ks == 1 ? 2 : 1));
+    for (int t = row_tiles(seqs[s].Lq, G, 256 / shape.ks) - 1; t >= 0; --t)
+      f((int)s, r0, t, tile_stages(seqs[s], G, shape, t, causal));
     r0 += (int64_t)((seqs[s].Lq + tpt - 1) / tpt) * 128;
   }
 }
 
-int choose_dq(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
+const Shape& choose_dq(const std::vector<Lengths>& seqs, int G, int Hkv, int causal) {
   std::vector<int> units;
-  int best = 1;
-  double best_est = 0.0;
-  for (int i = 0; i < 3; ++i) {
+  const Shape* best = kDqShapes;
+  double best_est = INFINITY;
+  for (const Shape& shape : kDqShapes) {
     int64_t stages = 0;
     units.clear();
-    each_dq(seqs, G, causal, kFwdParts[i], [&](int, int64_t, int, int st) {
+    each_dq(seqs, G, causal, shape, [&](int, int64_t, int, int st) {
       units.push_back(st);
       stages += st;
     });
-    const double limit = i == 0 ? INFINITY : best_est;
-    const double est = makespan(units, Hkv, kDqFixed, kDqStage[i], limit);
-    if (est < limit) {
-      best = kFwdParts[i];
+    const double est = shape_time(units, Hkv, shape, best_est);
+    if (est < best_est) {
+      best = &shape;
       best_est = est;
     }
-    if (i == 0 && est <= 1.1 * stages * Hkv * kDqStage[0] / kCUs) break;
+    if (shape.ks == 1 && est <= 1.1 * stages * Hkv * shape.stage / kCUs) break;
   }
-  return best;
+  return *best;
 }
 
 // Longest first, in the order they came.
@@ -348,7 +372,8 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
   h.total_k = cu_k[n];
 
   const FwdChoice c = choose_fwd(seqs, G, Hkv, causal);
-  h.fwd_ks = c.ks;
+  h.fwd_ks = c.shape->ks;
+  h.half = c.shape->half ? kHalfFwd : 0;
   // Partial rows: [parts][Lq][Hq] of every sequence that is cut.
   std::vector<int64_t> p0;
   int parts = 1;
@@ -399,10 +424,12 @@ int make_plan(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int Hkv, 
                              segs > 1 ? slot0[kb] + seg : -1});
            });
   longest_first(units, keys, &p->keys);
-  h.dq_ks = choose_dq(seqs, G, Hkv, causal);
+  const Shape& dq = choose_dq(seqs, G, Hkv, causal);
+  h.dq_ks = dq.ks;
+  if (dq.half) h.half |= kHalfDq;
   units.clear();
   std::vector<TileItem> dqs;
-  each_dq(seqs, G, causal, h.dq_ks, [&](int i, int64_t r0, int tile, int stages) {
+  each_dq(seqs, G, causal, dq, [&](int i, int64_t r0, int tile, int stages) {
     const Lengths& s = seqs[i];
     units.push_back(stages);
     dqs.push_back({s.q0, s.k0, r0, s.Lq, s.Lk, tile, 0});
@@ -543,7 +570,9 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
     a.Hkv = Hkv;
     a.G = Hq / Hkv;
     a.causal = h->causal;
-    UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsPlanned, h->fwd_ks, a, h->n_fwd, stream));
+    UPIPE_LAUNCH(kRowsFwd, stream,
+                 launch_rows_fwd(kRowsPlanned, h->fwd_ks, (h->half & kHalfFwd) != 0, a, h->n_fwd,
+                                 stream));
     if (h->n_merge > 0) {
       RowMergeArgs m{};
       m.part_o = a.part_o;
@@ -624,7 +653,9 @@ int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
     a.Hkv = Hkv;
     a.G = G;
     a.causal = h->causal;
-    if (h->n_dq > 0) UPIPE_LAUNCH(kRowsDq, stream, launch_rows_dq(h->dq_ks, a, h->n_dq, stream));
+    if (h->n_dq > 0)
+      UPIPE_LAUNCH(kRowsDq, stream,
+                   launch_rows_dq(h->dq_ks, (h->half & kHalfDq) != 0, a, h->n_dq, stream));
     if (h->n_key > 0) UPIPE_LAUNCH(kRowsDkdv, stream, launch_rows_dkdv(a, h->n_key, stream));
     if (h->n_fold > 0)
       UPIPE_LAUNCH(kRowsDkdvFold, stream, launch_rows_dkdv_fold(a, h->n_fold, stream));
@@ -692,13 +723,13 @@ constexpr double kCacheStage = 2.2, kFewStage = 2.0;
 void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
   double best = 0.0;
   for (int i = 0; i < 3; ++i) {
-    const int64_t n = (rows * kFwdParts[i] + 255) / 256 * Hkv;
+    const int64_t n = (rows * kFwdShapes[i].ks + 255) / 256 * Hkv;
     double est;
     const int parts = best_parts(n, (P + 127) / 128, 1, kCacheFixed, kPrefixStage[i],
-                                 kMergePart * (4.0 / kFwdParts[i]), &est);
+                                 kMergePart * (4.0 / kFwdShapes[i].ks), &est);
     if (i == 0 || est < best) {
       best = est;
-      p->prefix_ks = kFwdParts[i];
+      p->prefix_ks = kFwdShapes[i].ks;
       p->prefix_parts = parts;
     }
   }
@@ -790,7 +821,8 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
         !apart_cache(o, T, Hq, v, v_cache, B, cap, Hkv) ||
         (P > 0 && (!apart(o, T, Hq, k_prefix, P, Hkv) || !apart(o, T, Hq, v_prefix, P, Hkv))))
       return UPIPE_ERR_INVALID_ARG;
-    if (!stage_rows(k) || !stage_rows(v) || (P > 0 && (!stage_rows(k_prefix) || !stage_rows(v_prefix))))
+    if (!stage_rows(k) || !stage_rows(v) ||
+        (P > 0 && (!stage_rows(k_prefix) || !stage_rows(v_prefix))))
       return UPIPE_ERR_UNSUPPORTED;
     const CachePlan p = plan_cache(B, nq, cap, P, Hq, Hkv);
     if (ws_bytes < cache_ws(p)) return UPIPE_ERR_WORKSPACE;
@@ -835,7 +867,7 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     } else if (p.few) {
       UPIPE_LAUNCH(kRowsFwd, stream, launch_few_rows_fwd(a, blocks, stream));
     } else {
-      UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, a, blocks, stream));
+      UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, false, a, blocks, stream));
     }
     if (cache_parts(p) == 1) return UPIPE_OK;
     RowMergeArgs m{};

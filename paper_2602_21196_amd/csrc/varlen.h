@@ -51,6 +51,7 @@ struct TileItem {
   int32_t Lq, Lk, tile, pad;
 };
 
+enum Half { kHalfFwd = 1, kHalfDq = 2 };
 struct PlanHeader {
   uint64_t magic;
   int64_t bytes;                       // of the whole plan
@@ -59,9 +60,10 @@ struct PlanHeader {
   int64_t term_rows;                   // row terms of one key/value head
   int64_t slots;                       // segment sums of one key/value head
   int32_t Hq, Hkv, causal;
-  int32_t fwd_ks, dq_ks;               // key parts inside a workgroup
+  int32_t fwd_ks, dq_ks;               // 256 / rows of a workgroup: its key parts, unless half
   int32_t one_row;                     // of a merging workgroup
   int32_t n_fwd, n_merge, n_key, n_fold, n_dq;
+  int32_t half;                        // kHalfFwd | kHalfDq: workgroups of four waves
   int64_t at_fwd, at_merge, at_key, at_fold, at_dq;     // byte offsets
 };
 
@@ -84,7 +86,8 @@ struct RowFwdArgs {
 };
 enum RowMode { kRowsPlanned = 0, kRowsCache = 1, kRowsOne = 2 };
 // `blocks` items (of every key/value head).
-hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks, hipStream_t st);
+hipError_t launch_rows_fwd(int mode, int ks, bool half, const RowFwdArgs& a, int64_t blocks,
+                           hipStream_t st);
 
 // Caches with at most 32 packed rows (nq G) each: `blocks` as above, parts first.
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
@@ -125,6 +128,6 @@ struct RowBwdArgs {
 // n items of every key/value head.
 hipError_t launch_rows_dkdv(const RowBwdArgs& a, int64_t n, hipStream_t st);
 hipError_t launch_rows_dkdv_fold(const RowBwdArgs& a, int64_t n, hipStream_t st);
-hipError_t launch_rows_dq(int ks, const RowBwdArgs& a, int64_t n, hipStream_t st);
+hipError_t launch_rows_dq(int ks, bool half, const RowBwdArgs& a, int64_t n, hipStream_t st);
 
 }  // namespace upipe

@@ -7,7 +7,8 @@
 // products (as the matrix instructions take them), all sums are fp32.  The rows of
 // a key/value group are packed (varlen.h), so dK and dV sum over the group's heads by
 // walking its rows.  No atomics: every sum has a fixed order.
-//   dq:    a workgroup owns 256, 128 or 64 packed rows, forms their terms, D and
+//   dq:    a workgroup owns 256, 128 or 64 packed rows (or 128 with four waves, two of them
+//          a CU: the forward's reasons), forms their terms, D and
 //          -sqrt(d) lse, which it leaves for dkdv, and walks stages of keys
 //   dkdv:  a workgroup owns 128 keys of one key/value head and walks the tiles of
 //          rows that see them, from the last one down; long walks are cut into
@@ -258,17 +259,17 @@ __global__ __launch_bounds__(256) void rows_dkdv_fold_kernel(RowBwdArgs a) {
 // ---------------------------------------------------------------------- dQ
 // Eight waves of 32 packed rows x a part of every stage's keys: 256 rows x 64-key
 // stages, or, with the keys of 128-key stages in 2 or 4 parts, 128 or 64 rows, whose
-// sums are added in fp32 through LDS.
-template <int KS>
+// sums are added in fp32 through LDS.  Four waves: 128 rows x 64-key stages.
+template <int KS, int NW>
 struct DqTile {
-  static constexpr int NQW = 8 / KS;                // waves along the rows
+  static constexpr int NQW = NW / KS;               // waves along the rows
   static constexpr int BQ = 32 * NQW;               // rows per workgroup
   static constexpr int BK = KS == 1 ? 64 : 128;     // keys per stage
   static constexpr int NH = BK / 32 / KS;           // 32-key blocks of a stage per wave
   static constexpr int T = BK * HEAD_DIM * 2;
   static constexpr int OFF_K = 0, OFF_V = T;
   static constexpr int STAGE = 2 * T;
-  static constexpr int BLK = T / 1024 / 8;          // 1 KB blocks per wave per tensor
+  static constexpr int BLK = T / 1024 / NW;         // 1 KB blocks per wave per tensor
 };
 constexpr int DQ_LA = 4;     // K/V fragment reads kept in flight
 // D of the rows that see no more keys than these, one block of products, comes from
@@ -278,9 +279,9 @@ constexpr int DQ_LA = 4;     // K/V fragment reads kept in flight
 // 2.4e-3 off instead of 2.6e-3 (2.3e-3 are the roundings of dS and of the result).
 constexpr int kFewKeys = 32;
 
-template <int KS>
-__global__ __launch_bounds__(512, 1) void rows_dq_kernel(RowBwdArgs a) {
-  using T = DqTile<KS>;
+template <int KS, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void rows_dq_kernel(RowBwdArgs a) {
+  using T = DqTile<KS, NW>;
   __shared__ __attribute__((aligned(1024))) char smem[2 * T::STAGE];
   const int t = threadIdx.x;
   const int lane = t & 63;
@@ -500,9 +501,13 @@ hipError_t launch_rows_dkdv_fold(const RowBwdArgs& a, int64_t n, hipStream_t st)
   return enqueue(rows_dkdv_fold_kernel, dim3((unsigned)(n * 16), (unsigned)a.Hkv), 256, st, a);
 }
 
-hipError_t launch_rows_dq(int ks, const RowBwdArgs& a, int64_t n, hipStream_t st) {
-  return enqueue(ks == 1 ? rows_dq_kernel<1> : ks == 2 ? rows_dq_kernel<2> : rows_dq_kernel<4>,
-                 dim3((unsigned)(n * a.Hkv)), 512, st, a);
+hipError_t launch_rows_dq(int ks, bool half, const RowBwdArgs& a, int64_t n, hipStream_t st) {
+  const dim3 grid((unsigned)(n * a.Hkv));
+  if (half) return enqueue(rows_dq_kernel<1, 4>, grid, 256, st, a);
+  return enqueue(ks == 1   ? rows_dq_kernel<1, 8>
+                 : ks == 2 ? rows_dq_kernel<2, 8>
+                           : rows_dq_kernel<4, 8>,
+                 grid, 512, st, a);
 }
 
 }  // namespace upipe

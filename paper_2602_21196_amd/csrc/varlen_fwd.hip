@@ -9,7 +9,9 @@
 // pair, P in registers as the operand of O^T += V^T P^T; one pass with a running
 // reference maximum), with
 //   - rows packed by key/value group (varlen.h), KS parts of every stage's keys by a
-//     workgroup's waves: 256, 128 or 64 rows;
+//     workgroup's waves: 256, 128 or 64 rows; or, where many sequences are short,
+//     workgroups of four waves over 128 rows and stages of 64 keys, two a CU: one's loads
+//     of Q and stores of O hide behind the other's products;
 //   - one launch over a host-made list of tiles, longest first;
 //   - a tile's keys cut into parts where tiles are few: fp32 results, merged.
 // Up to 32 packed rows a cache have a kernel of their own (few_rows_kernel); a prefix and the
@@ -17,17 +19,22 @@
 // What bounds it: MFMA issue where tiles fill the chip (131072 tokens, 4 heads on 1: 14.2
 // ms, 1240 TFLOP/s, as the forward over equal lengths; 65536 tokens in documents of up to
 // 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 100 us,
-// 5.1 TB/s, 24 of 8192 5.4; a plain read of as much 5.4), launches and one chain of stages in short calls.
+// 5.1 TB/s, 24 of 8192 5.4; a plain read of as much 5.4), launches and one chain of
+// stages in short calls.
 #include "varlen.h"
 
 namespace upipe {
 
 namespace {
 
-constexpr int BKS = 128;       // keys per LDS stage
-constexpr int K_TILE = BKS * HEAD_DIM * 2;       // [128][128] bf16 = 32 KB
-constexpr int V_TILE = HEAD_DIM * BKS * 2;       // [128][128] bf16 = 32 KB
-constexpr int STAGE = K_TILE + V_TILE;
+// A workgroup of NW waves: 16 NW keys per LDS stage, so that every wave copies four rows
+// four times of K and of V.
+template <int NW>
+struct Stage {
+  static constexpr int KEYS = 16 * NW;
+  static constexpr int K_TILE = KEYS * HEAD_DIM * 2;      // 32 KB with 8 waves, and V as much
+  static constexpr int BYTES = 2 * K_TILE;
+};
 constexpr float kSumMax = 256.f;   // lazy-rescale bound on a lane's stage sum (2^8)
 // Reference max of a row before its first key (log2 domain): a finite stand-in for
 // -inf, below every finite score times log2(e) / sqrt(d), so that a stage whose keys are
@@ -331,10 +338,11 @@ __device__ __forceinline__ int nth_cache(const RowFwdArgs& a, int n, int& Lk) {
 
 // A workgroup: BQ packed rows of one key/value head against a range of its keys.  It is
 // number `block` of `blocks`, all heads'.
-template <int KS, int MODE>
+template <int KS, int MODE, int NW>
 __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int block, int blocks) {
-  constexpr int NQW = 8 / KS;            // waves along the rows
-  constexpr int NT = 4 / KS;             // 32-key tiles of a stage per wave
+  constexpr int BKS = Stage<NW>::KEYS, K_TILE = Stage<NW>::K_TILE, STAGE = Stage<NW>::BYTES;
+  constexpr int NQW = NW / KS;           // waves along the rows
+  constexpr int NT = BKS / 32 / KS;      // 32-key tiles of a stage per wave
   constexpr int BQ = 32 * NQW;           // rows per workgroup
   const int t = threadIdx.x;
   const int lane = t & 63;
@@ -480,10 +488,10 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
   write_row(a, part, it, part_rows, lse_at, tok, kvh * G + hg, Hq, g, oacc, m_ref, l_tot);
 }
 
-template <int KS, int MODE>
-__global__ __launch_bounds__(512, 1) void rows_fwd_kernel(RowFwdArgs a) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
-  rows_fwd<KS, MODE>(a, smem, blockIdx.x, gridDim.x);
+template <int KS, int MODE, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void rows_fwd_kernel(RowFwdArgs a) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * Stage<NW>::BYTES];
+  rows_fwd<KS, MODE, NW>(a, smem, blockIdx.x, gridDim.x);
 }
 
 // Up to 32 packed rows of one cache and key/value head: a wave takes every NW-th 32-key
@@ -636,11 +644,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs 
 template <int KS, bool FEW>
 __global__ __launch_bounds__(512, 1) void rows_prefix_kernel(RowFwdArgs p, RowFwdArgs c,
                                                              int n_cache) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * STAGE];
+  __shared__ __attribute__((aligned(1024))) char smem[2 * Stage<8>::BYTES];
   const int b = blockIdx.x;
-  if (b >= n_cache) rows_fwd<KS, kRowsOne>(p, smem, b - n_cache, gridDim.x - n_cache);
+  if (b >= n_cache) rows_fwd<KS, kRowsOne, 8>(p, smem, b - n_cache, gridDim.x - n_cache);
   else if (FEW) few_rows<4>(c, smem, b);
-  else rows_fwd<4, kRowsCache>(c, smem, b, n_cache);
+  else rows_fwd<4, kRowsCache, 8>(c, smem, b, n_cache);
 }
 
 // The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
@@ -762,12 +770,15 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
 
 }  // namespace
 
-hipError_t launch_rows_fwd(int mode, int ks, const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
-  return enqueue(mode == kRowsCache ? rows_fwd_kernel<4, kRowsCache>
-                 : ks == 1          ? rows_fwd_kernel<1, kRowsPlanned>
-                 : ks == 2          ? rows_fwd_kernel<2, kRowsPlanned>
-                                    : rows_fwd_kernel<4, kRowsPlanned>,
-                 dim3((unsigned)(blocks * a.Hkv)), 512, st, a);
+hipError_t launch_rows_fwd(int mode, int ks, bool half, const RowFwdArgs& a, int64_t blocks,
+                           hipStream_t st) {
+  const dim3 grid((unsigned)(blocks * a.Hkv));
+  if (half) return enqueue(rows_fwd_kernel<1, kRowsPlanned, 4>, grid, 256, st, a);
+  return enqueue(mode == kRowsCache ? rows_fwd_kernel<4, kRowsCache, 8>
+                 : ks == 1          ? rows_fwd_kernel<1, kRowsPlanned, 8>
+                 : ks == 2          ? rows_fwd_kernel<2, kRowsPlanned, 8>
+                                    : rows_fwd_kernel<4, kRowsPlanned, 8>,
+                 grid, 512, st, a);
 }
 
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
