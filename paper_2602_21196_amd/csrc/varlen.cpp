@@ -571,8 +571,7 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
     a.G = Hq / Hkv;
     a.causal = h->causal;
     UPIPE_LAUNCH(kRowsFwd, stream,
-                 launch_rows_fwd(kRowsPlanned, h->fwd_ks, (h->half & kHalfFwd) != 0, a, h->n_fwd,
-                                 stream));
+                 launch_rows_fwd(h->fwd_ks, (h->half & kHalfFwd) != 0, a, h->n_fwd, stream));
     if (h->n_merge > 0) {
       RowMergeArgs m{};
       m.part_o = a.part_o;
@@ -691,14 +690,15 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
   return grid_fits(P > 0 ? 2 * rows + 8192 : rows, 512) ? UPIPE_OK : UPIPE_ERR_UNSUPPORTED;
 }
 
-// Parts of at least `least` of the stages for n workgroups, expected to end first: rounds of
-// the chip, each of the fixed us of a workgroup and those of its stages, and the merge's
-// us of a part.
-int best_parts(int64_t n, int64_t stages, int64_t least, double fixed, double stage, double merge,
-               double* est) {
+// Parts of at least `least` of the stages for n workgroups, per_cu of them a CU, expected
+// to end first: rounds of the chip, each of the fixed us of a workgroup and those of its
+// stages, and the merge's us of a part.
+int best_parts(int64_t n, int per_cu, int64_t stages, int64_t least, double fixed, double stage,
+               double merge, double* est) {
+  const int64_t places = per_cu * kCUs;
   int best = 1;
   for (int64_t p = 1; p <= std::max<int64_t>(1, std::min<int64_t>(stages / least, 2 * kCUs)); ++p) {
-    const double t = (n * p + kCUs - 1) / kCUs * (fixed + (stages + p - 1) / p * stage) +
+    const double t = (n * p + places - 1) / places * (fixed + (stages + p - 1) / p * stage) +
                      merge * n * p;
     if (p == 1 || t < *est) {
       best = (int)p;
@@ -713,19 +713,21 @@ int best_parts(int64_t n, int64_t stages, int64_t least, double fixed, double st
 // workgroup besides (its rows of 16384 x 8 heads, 64 a sequence, 1 | 2 | 4: 64 sequences
 // 42 | 42 | 47 us, 256 sequences 142 | 150 | 179, 64 of one head of 8 rows 20 | 18 | 15).
 constexpr double kPrefixStage[3] = {4.2, 2.25, 1.3}, kCacheFixed = 8.0;
-// us of a stage of 64 rows of a cache, and of 32 with the prefix beside them: 64 caches of 900
-// rows, 128 packed rows each, without a prefix in 1 | 2 | 4 parts 20 | 17 + 7 | 27 + 8 us, 4
-// of 15000, 256 rows x 4 heads, 2 | 4 | 16 110 | 66 | 99; with one, 8 rows: one of 131071
-// in 128 | 256 parts 20 | 24, 24 of 1 to 16384, 8 heads 2 | 4 | 16 131 | 116 | 131, 64 of
-// 1 to 1024, 8 heads, 1 | 2 81 | 88.
-constexpr double kCacheStage = 2.2, kFewStage = 2.0;
+// us of 128 keys of 64 rows of a cache, two workgroups of four waves a CU, or one of eight
+// beside a prefix, and of up to 32 rows there.  In parts, us with the merge (one workgroup
+// of eight waves a CU in brackets): 4 caches of 15000 rows, 4 heads, 256 packed rows each,
+// in 4 | 8 | 16 84 | 63 | 76 (73 in 4); 24 of 8192, 8 heads, 36 rows, in 2 | 5 | 8 170 |
+// 170 | 179 (180 in 5), of 1 to 16384 in 4 | 8 | 12 139 | 124 | 132 (126 in 4).  Behind a
+// prefix, 8 rows: one of 131071 in 128 | 256 parts 20 | 24, 24 of 1 to 16384, 8 heads 2 |
+// 4 | 16 131 | 116 | 131, 64 of 1 to 1024, 8 heads, 1 | 2 81 | 88.
+constexpr double kHalfStage = 2.8, kCacheStage = 2.2, kFewStage = 2.0;
 
 void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
   double best = 0.0;
   for (int i = 0; i < 3; ++i) {
     const int64_t n = (rows * kFwdShapes[i].ks + 255) / 256 * Hkv;
     double est;
-    const int parts = best_parts(n, (P + 127) / 128, 1, kCacheFixed, kPrefixStage[i],
+    const int parts = best_parts(n, 1, (P + 127) / 128, 1, kCacheFixed, kPrefixStage[i],
                                  kMergePart * (4.0 / kFwdShapes[i].ks), &est);
     if (i == 0 || est < best) {
       best = est;
@@ -768,9 +770,10 @@ CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv)
   const int64_t groups = B * Hkv * (p.few ? 1 : (nq * G + 63) / 64);
   double est;
   if (!p.few)
-    p.splits = best_parts(groups, stages, 4, kCacheFixed, kCacheStage, kMergePart, &est);
+    p.splits = best_parts(groups, P > 0 ? 1 : 2, stages, 4, kCacheFixed,
+                          P > 0 ? kCacheStage : kHalfStage, kMergePart, &est);
   else if (P > 0)
-    p.splits = best_parts(groups, stages, 8, kCacheFixed, kFewStage, kMergePart, &est);
+    p.splits = best_parts(groups, 1, stages, 8, kCacheFixed, kFewStage, kMergePart, &est);
   else
     p.splits = few_parts(groups, cap);
   if (P > 0) plan_prefix(B * nq * G, P, Hkv, &p);
@@ -853,7 +856,7 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     // once and are not so many that they even each other out.  us in an order of chance | the
     // longest last, as they come and ranked: 24 caches of 1 to 16384 rows, 8 heads 110 | 114
     // and 103, with 9 new tokens 138 | 135 and 118; 64 of them 130 | 146 and 139.
-    a.ranked = B <= 64 && B * Hkv <= kCUs && blocks * Hkv > (p.few && P == 0 ? 2 : 1) * kCUs;
+    a.ranked = B <= 64 && B * Hkv <= kCUs && blocks * Hkv > (P == 0 ? 2 : 1) * kCUs;
     if (P > 0) {
       one.k = view_of(k_prefix);
       one.v = view_of(v_prefix);
@@ -867,7 +870,7 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     } else if (p.few) {
       UPIPE_LAUNCH(kRowsFwd, stream, launch_few_rows_fwd(a, blocks, stream));
     } else {
-      UPIPE_LAUNCH(kRowsFwd, stream, launch_rows_fwd(kRowsCache, 4, false, a, blocks, stream));
+      UPIPE_LAUNCH(kRowsFwd, stream, launch_cache_rows_fwd(a, blocks, stream));
     }
     if (cache_parts(p) == 1) return UPIPE_OK;
     RowMergeArgs m{};

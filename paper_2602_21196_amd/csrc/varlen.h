@@ -85,11 +85,13 @@ struct RowFwdArgs {
   bool ranked;               // caches: the longest first
 };
 enum RowMode { kRowsPlanned = 0, kRowsCache = 1, kRowsOne = 2 };
-// `blocks` items (of every key/value head).
-hipError_t launch_rows_fwd(int mode, int ks, bool half, const RowFwdArgs& a, int64_t blocks,
-                           hipStream_t st);
+// Planned sequences: `blocks` items (of every key/value head).
+hipError_t launch_rows_fwd(int ks, bool half, const RowFwdArgs& a, int64_t blocks, hipStream_t st);
 
-// Caches with at most 32 packed rows (nq G) each: `blocks` as above, parts first.
+// Caches, by tiles of 64 packed rows: `blocks` tiles of every key/value head, parts first.
+hipError_t launch_cache_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
+
+// Caches with at most 32 packed rows (nq G) each.
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
 
 // The same caches behind a prefix (p), both in one launch.

@@ -770,15 +770,17 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
 
 }  // namespace
 
-hipError_t launch_rows_fwd(int mode, int ks, bool half, const RowFwdArgs& a, int64_t blocks,
-                           hipStream_t st) {
+hipError_t launch_rows_fwd(int ks, bool half, const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
   const dim3 grid((unsigned)(blocks * a.Hkv));
   if (half) return enqueue(rows_fwd_kernel<1, kRowsPlanned, 4>, grid, 256, st, a);
-  return enqueue(mode == kRowsCache ? rows_fwd_kernel<4, kRowsCache, 8>
-                 : ks == 1          ? rows_fwd_kernel<1, kRowsPlanned, 8>
-                 : ks == 2          ? rows_fwd_kernel<2, kRowsPlanned, 8>
-                                    : rows_fwd_kernel<4, kRowsPlanned, 8>,
+  return enqueue(ks == 1   ? rows_fwd_kernel<1, kRowsPlanned, 8>
+                 : ks == 2 ? rows_fwd_kernel<2, kRowsPlanned, 8>
+                           : rows_fwd_kernel<4, kRowsPlanned, 8>,
                  grid, 512, st, a);
+}
+
+hipError_t launch_cache_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
+  return enqueue(rows_fwd_kernel<2, kRowsCache, 4>, dim3((unsigned)(blocks * a.Hkv)), 256, st, a);
 }
 
 hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
