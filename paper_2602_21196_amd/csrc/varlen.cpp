@@ -673,7 +673,6 @@ namespace {
 
 // How a call over caches is cut: key parts of every row, and of the prefix.
 struct CachePlan {
-  bool few = false;        // at most 32 packed rows of a cache
   int splits = 1;
   int prefix_ks = 1, prefix_parts = 0;
   int64_t rows = 0;        // B * nq * Hq
@@ -690,56 +689,66 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
   return grid_fits(P > 0 ? 2 * rows + 8192 : rows, 512) ? UPIPE_OK : UPIPE_ERR_UNSUPPORTED;
 }
 
-// Parts of at least `least` of the stages for n workgroups, per_cu of them a CU, expected
-// to end first: rounds of the chip, each of the fixed us of a workgroup and those of its
-// stages, and the merge's us of a part.
-int best_parts(int64_t n, int per_cu, int64_t stages, int64_t least, double fixed, double stage,
-               double merge, double* est) {
-  const int64_t places = per_cu * kCUs;
-  int best = 1;
-  for (int64_t p = 1; p <= std::max<int64_t>(1, std::min<int64_t>(stages / least, 2 * kCUs)); ++p) {
-    const double t = (n * p + places - 1) / places * (fixed + (stages + p - 1) / p * stage) +
-                     merge * n * p;
-    if (p == 1 || t < *est) {
-      best = (int)p;
-      *est = t;
-    }
-  }
-  return best;
-}
+// us of a cache's workgroup besides its stages, and of 128 keys of 64 rows with two
+// workgroups a CU.
+constexpr double kCacheFixed = 8.0, kCacheStage = 2.8;
 
-// The prefix's workgroups: 256, 128 or 64 packed rows (1, 2 or 4 key parts inside)
-// against one of some parts of it.  us of a stage and of a
-// workgroup besides (its rows of 16384 x 8 heads, 64 a sequence, 1 | 2 | 4: 64 sequences
-// 42 | 42 | 47 us, 256 sequences 142 | 150 | 179, 64 of one head of 8 rows 20 | 18 | 15).
-constexpr double kPrefixStage[3] = {4.2, 2.25, 1.3}, kCacheFixed = 8.0;
-// us of 128 keys of 64 rows of a cache, two workgroups of four waves a CU, or one of eight
-// beside a prefix, and of up to 32 rows there.  In parts, us with the merge (one workgroup
-// of eight waves a CU in brackets): 4 caches of 15000 rows, 4 heads, 256 packed rows each,
-// in 4 | 8 | 16 84 | 63 | 76 (73 in 4); 24 of 8192, 8 heads, 36 rows, in 2 | 5 | 8 170 |
-// 170 | 179 (180 in 5), of 1 to 16384 in 4 | 8 | 12 139 | 124 | 132 (126 in 4).  Behind a
-// prefix, 8 rows: one of 131071 in 128 | 256 parts 20 | 24, 24 of 1 to 16384, 8 heads 2 |
-// 4 | 16 131 | 116 | 131, 64 of 1 to 1024, 8 heads, 1 | 2 81 | 88.
-constexpr double kHalfStage = 2.8, kCacheStage = 2.2, kFewStage = 2.0;
-
-void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
+// Parts of caches of more than 32 packed rows, 4 stages at least, expected to end first:
+// rounds of the chip, two workgroups a CU, and the merge's us of a part.  us with the merge:
+// 4 caches of 15000 rows, 4 heads, 256 packed rows each, in 4 | 8 | 16 84 | 63 | 76; 24 of
+// 8192, 8 heads, 36 rows, in 2 | 5 | 8 170 | 170 | 179, of 1 to 16384 in 4 | 8 | 12 139 |
+// 124 | 132.
+int tile_parts(int64_t groups, int64_t cap) {
+  const int64_t places = 2 * kCUs, stages = (cap + 127) / 128;
   double best = 0.0;
-  for (int i = 0; i < 3; ++i) {
-    const int64_t n = (rows * kFwdShapes[i].ks + 255) / 256 * Hkv;
-    double est;
-    const int parts = best_parts(n, 1, (P + 127) / 128, 1, kCacheFixed, kPrefixStage[i],
-                                 kMergePart * (4.0 / kFwdShapes[i].ks), &est);
-    if (i == 0 || est < best) {
-      best = est;
-      p->prefix_ks = kFwdShapes[i].ks;
-      p->prefix_parts = parts;
+  int parts = 1;
+  for (int64_t p = 1; p <= std::max<int64_t>(1, std::min<int64_t>(stages / 4, places)); ++p) {
+    const double t = (groups * p + places - 1) / places *
+                         (kCacheFixed + (stages + p - 1) / p * kCacheStage) +
+                     kMergePart * groups * p;
+    if (p == 1 || t < best) {
+      best = t;
+      parts = (int)p;
+    }
+  }
+  return parts;
+}
+
+// The prefix's workgroups: 128 or 64 packed rows (1 or 2 key parts inside) against one of
+// some parts of it.  us of 64 keys of the only one on a CU and of one of two, and of a
+// workgroup besides; a merge reads every part.  Up to one a CU leaves room for the
+// caches' (`caches` us, half full), more of them push those behind.  us with the merge
+// (in brackets by eight waves of 256 rows and caches first): 64 caches of 1 to 1024 rows, 64
+// heads on 8, behind 16384, 128 rows in 4 | 8 | 16 parts 108 | 75 | 91 (91), 64 rows in 8 94;
+// 64 of 200 behind 4096 in 4 | 8 | 16 39 | 38 | 47 (50), 64 rows in 4 36; 200 of 900 behind
+// 32768 in 2 | 4 | 8 381 | 334 | 361 (405).
+constexpr double kPrefixAlone[2] = {1.4, 1.1}, kPrefixBoth[2] = {2.3, 1.7};
+
+void plan_prefix(int64_t rows, int64_t P, int Hkv, double caches, CachePlan* p) {
+  const int64_t stages = (P + 63) / 64;
+  double best = INFINITY;
+  for (int ks = 1; ks <= 2; ++ks) {
+    const double alone = kPrefixAlone[ks - 1], both = kPrefixBoth[ks - 1];
+    const int64_t n = (rows * ks + 127) / 128 * Hkv;
+    for (int64_t parts = 1; parts <= std::min<int64_t>(stages, 2 * kCUs); ++parts) {
+      const int64_t w = n * parts, rest = w % (2 * kCUs), st = (stages + parts - 1) / parts;
+      const double more = std::max(0.0, (double)(rest - kCUs) / kCUs);
+      double t = w / (2 * kCUs) * (kCacheFixed + st * both) + kMergePart * (2.0 / ks) * w;
+      if (rest > 0) t += kCacheFixed + st * (alone + more * (both - alone));
+      if (w > kCUs) t += caches;
+      if (t < best) {
+        best = t;
+        p->prefix_ks = ks;
+        p->prefix_parts = (int)parts;
+      }
     }
   }
 }
 
-// Parts for few_rows_kernel, two workgroups a CU: of 1024 rows, unless they are more than
-// four a CU, or of 2048, unless they are more than sixteen; or up to twice as many (512
-// rows each at least) where that fills the chip, or whole rounds of it, better.  us with the
+// Parts of caches of up to 32 packed rows, which wait for memory alone: of 1024 rows, unless
+// they are more than four a CU, or of 2048, unless they are more than sixteen; or up to
+// twice as many (512 rows each at least) where that fills the chip, two workgroups a
+// CU, or whole rounds of it, better.  us with the
 // merge: 24 caches of 8192 rows, 8 heads, in 5 | 6 | 8 parts 153 | 172 | 156, of 1 to 16384
 // in 4 | 6 | 8 | 12 122 | 119 | 116 | 119; 64 of 1 to 16384 in 2 | 4 | 8 | 16 172 | 148 |
 // 139 | 154, 8 in 4 | 8 | 16 | 32 62 | 40 | 32 | 38; 40 of 8000, 2 heads, in 4 | 6 | 8 |
@@ -747,7 +756,8 @@ void plan_prefix(int64_t rows, int64_t P, int Hkv, CachePlan* p) {
 // 113; one of 131072, parts of 256 | 512 | 1024 rows 48 | 37 | 33 before the merge had its
 // loads under way together, 23 with 512.
 int few_parts(int64_t groups, int64_t cap) {
-  const int64_t slots = 2 * kCUs, most = std::min<int64_t>((cap + 511) / 512, kMostParts);
+  const int64_t slots = 2 * kCUs;
+  const int64_t most = std::min((cap + 511) / 512, kMostParts - slots);     // and a prefix's
   const int64_t least =
       std::min(most, std::max({int64_t(1), std::min((cap + 1023) / 1024, 2 * slots / groups),
                                std::min((cap + 2047) / 2048, 8 * slots / groups)}));
@@ -759,24 +769,14 @@ int few_parts(int64_t groups, int64_t cap) {
 }
 
 // The lengths are on the device: the cut goes by the capacity, and a part is the same
-// share of whatever a cache holds.  Up to 32 packed rows a cache go by few_rows_kernel (64
-// caches of 512 rows, 8 heads of 8 rows: 25 us, by the tiles of 64 rows 37; one of 131071
-// rows 16.5 and 17).
+// share of whatever a cache holds.
 CachePlan plan_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv) {
   CachePlan p;
   p.rows = B * nq * Hq;
-  const int64_t G = Hq / Hkv, stages = (cap + 127) / 128;
-  p.few = nq * G <= 32;
-  const int64_t groups = B * Hkv * (p.few ? 1 : (nq * G + 63) / 64);
-  double est;
-  if (!p.few)
-    p.splits = best_parts(groups, P > 0 ? 1 : 2, stages, 4, kCacheFixed,
-                          P > 0 ? kCacheStage : kHalfStage, kMergePart, &est);
-  else if (P > 0)
-    p.splits = best_parts(groups, 1, stages, 8, kCacheFixed, kFewStage, kMergePart, &est);
-  else
-    p.splits = few_parts(groups, cap);
-  if (P > 0) plan_prefix(B * nq * G, P, Hkv, &p);
+  const int64_t G = Hq / Hkv, groups = B * Hkv * ((nq * G + 63) / 64);
+  p.splits = nq * G > 32 ? tile_parts(groups, cap) : few_parts(groups, cap);
+  // half of the caches' bytes at 5.3 TB/s
+  if (P > 0) plan_prefix(B * nq * G, P, Hkv, B * Hkv * (cap / 2) * 512 / 5.3e6, &p);
   return p;
 }
 
@@ -851,24 +851,22 @@ int upipe_attn_decode(upipe_heads q, upipe_heads k, int64_t k_cache, upipe_heads
     a.splits = p.splits;
     a.part0 = p.prefix_parts;
     a.lse_head = nq;
-    const int64_t blocks = (p.few ? 1 : ((int64_t)nq * G + 63) / 64) * B * p.splits;
-    // The longest first, for a microsecond of every workgroup, where they do not all start at
-    // once and are not so many that they even each other out.  us in an order of chance | the
+    const int64_t blocks = ((int64_t)nq * G + 63) / 64 * B * p.splits;
+    // The longest first, for some time of every workgroup, where they do not all start at once
+    // and are not so many that they even each other out.  us in an order of chance | the
     // longest last, as they come and ranked: 24 caches of 1 to 16384 rows, 8 heads 110 | 114
-    // and 103, with 9 new tokens 138 | 135 and 118; 64 of them 130 | 146 and 139.
-    a.ranked = B <= 64 && B * Hkv <= kCUs && blocks * Hkv > (P == 0 ? 2 : 1) * kCUs;
+    // and 102, with 9 new tokens 138 | 135 and 118; 64 of them 130 | 146 and 139.
+    a.ranked = B <= 64 && B * Hkv <= kCUs && blocks * Hkv > 2 * kCUs;
     if (P > 0) {
       one.k = view_of(k_prefix);
       one.v = view_of(v_prefix);
       one.one.Lq = (int32_t)T;
       one.one.Lk = (int32_t)P;
       one.one.parts = p.prefix_parts;
-      const int64_t tiles = (T * G * p.prefix_ks + 255) / 256;
+      const int64_t tiles = (T * G * p.prefix_ks + 127) / 128;
       UPIPE_LAUNCH(kRowsFwd, stream,
-                   launch_rows_prefix(p.prefix_ks, p.few, one, a, tiles * p.prefix_parts, blocks,
+                   launch_rows_prefix(p.prefix_ks, one, a, tiles, blocks,
                                       stream));
-    } else if (p.few) {
-      UPIPE_LAUNCH(kRowsFwd, stream, launch_few_rows_fwd(a, blocks, stream));
     } else {
       UPIPE_LAUNCH(kRowsFwd, stream, launch_cache_rows_fwd(a, blocks, stream));
     }

@@ -91,12 +91,10 @@ hipError_t launch_rows_fwd(int ks, bool half, const RowFwdArgs& a, int64_t block
 // Caches, by tiles of 64 packed rows: `blocks` tiles of every key/value head, parts first.
 hipError_t launch_cache_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
 
-// Caches with at most 32 packed rows (nq G) each.
-hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st);
-
-// The same caches behind a prefix (p), both in one launch.
-hipError_t launch_rows_prefix(int ks, bool few, const RowFwdArgs& p, const RowFwdArgs& c,
-                              int64_t prefix_blocks, int64_t cache_blocks, hipStream_t st);
+// The same caches behind a prefix (p, its rows in so many tiles of 128 / ks), both in one
+// launch.
+hipError_t launch_rows_prefix(int ks, const RowFwdArgs& p, const RowFwdArgs& c, int64_t tiles,
+                              int64_t cache_blocks, hipStream_t st);
 
 struct RowMergeArgs {
   const float *part_o, *part_lse;

@@ -14,8 +14,8 @@
 //     of Q and stores of O hide behind the other's products;
 //   - one launch over a host-made list of tiles, longest first;
 //   - a tile's keys cut into parts where tiles are few: fp32 results, merged.
-// Up to 32 packed rows a cache have a kernel of their own (few_rows_kernel); a prefix and the
-// caches behind it share a launch (rows_prefix_kernel).
+// Caches go by workgroups of four waves too, two a CU, 64 rows each; a prefix and the caches
+// behind it share a launch, so that the products of the one hide the other's loads.
 // What bounds it: MFMA issue where tiles fill the chip (131072 tokens, 4 heads on 1: 14.2
 // ms, 1240 TFLOP/s, as the forward over equal lengths; 65536 tokens in documents of up to
 // 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 100 us,
@@ -336,10 +336,10 @@ __device__ __forceinline__ int nth_cache(const RowFwdArgs& a, int n, int& Lk) {
   return b;
 }
 
-// A workgroup: BQ packed rows of one key/value head against a range of its keys.  It is
-// number `block` of `blocks`, all heads'.
+// A workgroup: BQ packed rows of one key/value head against a range of its keys; number
+// `block` of a launch's.
 template <int KS, int MODE, int NW>
-__device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int block, int blocks) {
+__device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int block) {
   constexpr int BKS = Stage<NW>::KEYS, K_TILE = Stage<NW>::K_TILE, STAGE = Stage<NW>::BYTES;
   constexpr int NQW = NW / KS;           // waves along the rows
   constexpr int NT = BKS / 32 / KS;      // 32-key tiles of a stage per wave
@@ -349,11 +349,9 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
   const int w = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wq = KS == 1 ? w : w % NQW, ks = KS == 1 ? 0 : w / NQW;
   const int r32 = lane & 31, g = lane >> 5;
-  const int G = a.G, Hq = a.Hkv * G, items = blocks / a.Hkv;
-  // A prefix's parts go round the XCDs, not its heads: an XCD that reads one head of
-  // eight, 256 bytes out of every 2 KB, uses two of its L2's sixteen channels.
-  const int kvh = MODE == kRowsOne ? block / items : block % a.Hkv;
-  const int idx = MODE == kRowsOne ? block % items : block / a.Hkv;
+  const int G = a.G, Hq = a.Hkv * G;
+  int kvh = block % a.Hkv;
+  const int idx = block / a.Hkv;
 
   RowItem it;
   int64_t cache = 0, lse_at, part_rows;
@@ -362,9 +360,14 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
     lse_at = it.q0;
     part_rows = (int64_t)it.Lq * Hq;
   } else if (MODE == kRowsOne) {
+    // The tiles that share a part of a head's keys on one XCD (blocks go round the eight)
+    // one after another; parts that there are not end at once.
     it = a.one;
-    it.part = idx % it.parts;
-    it.tile = idx / it.parts;
+    const int tiles = (it.Lq * G + BQ - 1) / BQ, u = block / (8 * tiles) * 8 + (block & 7);
+    if (u >= a.Hkv * it.parts) return;
+    it.tile = block / 8 % tiles;
+    kvh = u / it.parts;
+    it.part = u % it.parts;
     lse_at = 0;                  // always parts
     part_rows = (int64_t)it.Lq * Hq;
   } else {
@@ -491,164 +494,18 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
 template <int KS, int MODE, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void rows_fwd_kernel(RowFwdArgs a) {
   __shared__ __attribute__((aligned(1024))) char smem[2 * Stage<NW>::BYTES];
-  rows_fwd<KS, MODE, NW>(a, smem, blockIdx.x, gridDim.x);
+  rows_fwd<KS, MODE, NW>(a, smem, blockIdx.x);
 }
 
-// Up to 32 packed rows of one cache and key/value head: a wave takes every NW-th 32-key
-// tile of the workgroup's part, each by itself: it copies its tile's K and V rows into
-// its own LDS, two tiles deep, waits for its own copies and meets the other waves only at
-// the end.  No barrier in the walk, and two workgroups a CU, so that one's start and end
-// hide behind the other's stream.  Beside a prefix, whose workgroups have a CU each, four
-// waves of eight do the same.
-constexpr int kFewWaves = 2;
-constexpr int kFewTile = 32 * HEAD_DIM * 2;        // K or V rows of a tile: 8 KB
-
-template <int NW>
-__device__ __forceinline__ void few_rows(const RowFwdArgs& a, char* smem, int block) {
-  const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r32 = lane & 31, g = lane >> 5;
-  if (w >= NW) return;
-  const int kvh = block % a.Hkv, idx = block / a.Hkv, G = a.G, Hq = a.Hkv * G;
-  int Lk;
-  const int b = nth_cache(a, idx / a.splits, Lk);
-  RowItem it{};
-  it.part = idx % a.splits;
-  it.q0 = (int64_t)b * a.nq;
-  it.p0 = it.q0 * Hq;
-  const int n_rows = a.nq * G, delta = Lk - a.nq;
-  const bool row_ok = r32 < n_rows;
-  const int tok = r32 / G, hg = r32 - tok * G;
-
-  const bf16* kp = a.k.p + b * a.k.batch + kvh * a.k.head;
-  const bf16* vp = a.v.p + b * a.v.batch + kvh * a.v.head;
-  const uint32_t k_row = (uint32_t)(a.k.row * 2), v_row = (uint32_t)(a.v.row * 2);
-  // Four blocks of four rows; the other four lie 16 rows on, swizzled alike.
-  uint32_t offk[4], offv[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 4 * i + (lane >> 4);
-    offk[i] = r * k_row + ((uint32_t)((lane & 15) ^ r) << 4);
-    offv[i] = r * v_row + (((lane & 15) ^ tsw(r)) << 4);
-  }
-  // Every row's keys end by Lk; this part's tiles, and this wave's of them.
-  const int tiles = (Lk + 31) / 32, per = (tiles + a.splits - 1) / a.splits;
-  const int t0 = min(tiles, per * it.part), t1 = min(tiles, t0 + per);
-  const uint32_t lds = lds_address(smem) + w * 4 * kFewTile;
-  auto copy = [&](int t, uint32_t to) {
-    // 16 rows from row r on, those past the last key as zeros
-    auto source = [&](const bf16* p, int64_t row, int r) {
-      const int n = t < t1 ? min(16, Lk - r) : 0;
-      return rsrc_words(p + r * row, n > 0 ? (uint32_t)((n - 1) * (int)row + HEAD_DIM) * 2 : 0);
-    };
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int r = 32 * t + 16 * half;
-      copy4_b128(source(kp, a.k.row, r), offk, 0, to + 4096 * half);
-      copy4_b128(source(vp, a.v.row, r), offv, 0, to + kFewTile + 4096 * half);
-    }
-  };
-  copy(t0 + w, lds);
-  copy(t0 + w + NW, lds + 2 * kFewTile);
-
-  bf16x8 qf[8];
-#pragma unroll
-  for (int s = 0; s < 8; ++s)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) qf[s][e] = (bf16)0.f;
-  if (row_ok) {
-    const bf16* qp = a.q.p + (it.q0 + tok) * a.q.row + (kvh * G + hg) * a.q.head + 8 * g;
-#pragma unroll
-    for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 16 * s);
-  }
-  f32x16 oacc[4];
-#pragma unroll
-  for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-  float m_ref = kNoMax, l_run = 0.f;
-  const int lim = min(tok + delta, Lk - 1), lim_w = delta;      // of token 0
-  const uint32_t k_lane = swz256(r32, g), v_lane = kFewTile + tr_base(lane);
-  // The queries are here before the walk (the compiler waits for them and, with them, for
-  // the first copies): within it, it would wait for every copy.
-#pragma unroll
-  for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(qf[s]));
-  for (int t = t0 + w, n = 0; t < t1; t += NW, ++n) {
-    const uint32_t boff = (w * 4 + 2 * (n & 1)) * kFewTile;
-    // This tile's 16 copies have landed; the next one's may be under way.
-    asm volatile("s_waitcnt vmcnt(16)" ::: "memory");
-    fwd_stage<1>(smem, k_lane + boff, v_lane + boff, 32 * t, lane, qf, lim, lim_w, oacc, m_ref,
-                 l_run, []() {}, []() {});
-    // Every read of the tile is done: its place takes the copies of the next but one.
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    copy(t + 2 * NW, lds_address(smem) + boff);
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the last, empty copies have ended
-  float l_tot = l_run + __shfl_xor(l_run, 32);
-  // The waves' parts folded in fp32, in their order, through LDS.
-  float* fold = reinterpret_cast<float*>(smem);
-  __syncthreads();
-  if (w > 0) {
-    float* mine = fold + (w - 1) * (4096 + 128) + lane * 4;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f32x4 v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = oacc[dt][4 * i + e];
-        *reinterpret_cast<f32x4*>(mine + (4 * dt + i) * 256) = v;
-      }
-    fold[(w - 1) * (4096 + 128) + 4096 + lane] = m_ref;
-    fold[(w - 1) * (4096 + 128) + 4096 + 64 + lane] = l_tot;
-  }
-  __syncthreads();
-  if (w > 0) return;
-#pragma unroll
-  for (int p = 0; p < NW - 1; ++p) {
-    const float* part = fold + p * (4096 + 128);
-    const float m_p = part[4096 + lane], l_p = part[4096 + 64 + lane];
-    const float m_new = fmaxf(m_ref, m_p);
-    const float a0 = fast_exp2(m_ref - m_new), a1 = fast_exp2(m_p - m_new);
-    m_ref = m_new;
-    l_tot = l_tot * a0 + l_p * a1;
-#pragma unroll
-    for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(part + (4 * dt + i) * 256 + lane * 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          oacc[dt][4 * i + e] = oacc[dt][4 * i + e] * a0 + v[e] * a1;
-      }
-  }
-  mend_row(row_ok, kp, a.k.row, vp, a.v.row, 32 * t0, min(lim + 1, 32 * t1), lim,
-           min(Lk, 32 * t1), qf, g, oacc, m_ref, l_tot);
-  if (!row_ok) return;
-  it.part += a.part0;
-  write_row(a, a.splits + a.part0 > 1, it, (int64_t)a.B * a.nq * Hq, it.p0, tok, kvh * G + hg,
-            Hq, g, oacc, m_ref, l_tot);
-}
-
-__global__ __launch_bounds__(64 * kFewWaves, 1) void few_rows_kernel(RowFwdArgs a) {
-  __shared__ __attribute__((aligned(1024))) char smem[kFewWaves * 4 * kFewTile];
-  few_rows<kFewWaves>(a, smem, blockIdx.x);
-}
-
-// A shared prefix and the caches behind it in one launch, n_cache workgroups of the caches
-// first: they wait for memory, and the prefix's first ones start where they end.  Against
-// one launch each, without the merge, us: 64 caches of 1 to 1024 rows on 16384, 64 heads
-// on 8 80 | 86; 200 of 900 on 32768 359 | 415; 64 of 200 on 4096 41 | 41; 8 of 900 on
-// 2048, 8 heads on 1 12 | 23; the prefix first 86, 376, 41, 12, both by turns 92, 398,
-// 46, 12.
-template <int KS, bool FEW>
-__global__ __launch_bounds__(512, 1) void rows_prefix_kernel(RowFwdArgs p, RowFwdArgs c,
-                                                             int n_cache) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * Stage<8>::BYTES];
+// A shared prefix and the caches behind it in one launch, the prefix's workgroups first: of
+// the two on a CU one may wait for memory while the other multiplies.
+template <int KS>
+__global__ __launch_bounds__(256, 2) void rows_prefix_kernel(RowFwdArgs p, RowFwdArgs c,
+                                                             int n_prefix) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * Stage<4>::BYTES];
   const int b = blockIdx.x;
-  if (b >= n_cache) rows_fwd<KS, kRowsOne, 8>(p, smem, b - n_cache, gridDim.x - n_cache);
-  else if (FEW) few_rows<4>(c, smem, b);
-  else rows_fwd<4, kRowsCache, 8>(c, smem, b, n_cache);
+  if (b < n_prefix) rows_fwd<KS, kRowsOne, 4>(p, smem, b);
+  else rows_fwd<2, kRowsCache, 4>(c, smem, b - n_prefix);
 }
 
 // The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
@@ -783,20 +640,11 @@ hipError_t launch_cache_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_
   return enqueue(rows_fwd_kernel<2, kRowsCache, 4>, dim3((unsigned)(blocks * a.Hkv)), 256, st, a);
 }
 
-hipError_t launch_few_rows_fwd(const RowFwdArgs& a, int64_t blocks, hipStream_t st) {
-  return enqueue(few_rows_kernel, dim3((unsigned)(blocks * a.Hkv)), 64 * kFewWaves, st, a);
-}
-
-hipError_t launch_rows_prefix(int ks, bool few, const RowFwdArgs& p, const RowFwdArgs& c,
-                              int64_t prefix_blocks, int64_t cache_blocks, hipStream_t st) {
-  const int n_cache = (int)(cache_blocks * c.Hkv);
-  return enqueue(few ? (ks == 1   ? rows_prefix_kernel<1, true>
-                        : ks == 2 ? rows_prefix_kernel<2, true>
-                                  : rows_prefix_kernel<4, true>)
-                     : (ks == 1   ? rows_prefix_kernel<1, false>
-                        : ks == 2 ? rows_prefix_kernel<2, false>
-                                  : rows_prefix_kernel<4, false>),
-                 dim3((unsigned)(prefix_blocks * p.Hkv + n_cache)), 512, st, p, c, n_cache);
+hipError_t launch_rows_prefix(int ks, const RowFwdArgs& p, const RowFwdArgs& c, int64_t tiles,
+                              int64_t cache_blocks, hipStream_t st) {
+  const int n_prefix = (int)((p.Hkv * p.one.parts + 7) / 8 * 8 * tiles);
+  return enqueue(ks == 1 ? rows_prefix_kernel<1> : rows_prefix_kernel<2>,
+                 dim3((unsigned)(n_prefix + cache_blocks * c.Hkv)), 256, st, p, c, n_prefix);
 }
 
 hipError_t launch_rows_merge(const RowMergeArgs& a, int64_t items, hipStream_t st) {

@@ -208,8 +208,8 @@ def test_binding_refuses():
         upipe.attn_decode(torch.zeros((2, 3, 4, D), dtype=torch.bfloat16)[:, :2], c, c, n)
 
 
-# A prefix and caches in one launch: 1, 2 and 4 key parts of the prefix's rows, the caches by
-# tiles of 64 packed rows or as up to 32 of them.
+# A prefix and caches in one launch: tiles of 128 and 64 of the prefix's rows, of 64 packed
+# rows of the caches.
 BEHIND = [  # B, lens up to, cap, nq, Hq, Hkv, P
     (2, 300, 1000, 40, 8, 2, 700),
     (3, 2000, 2048, 16, 16, 2, 3000),
