@@ -692,6 +692,8 @@ int check_cache(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv, int 
 // us of a cache's workgroup besides its stages, and of 128 keys of 64 rows with two
 // workgroups a CU.
 constexpr double kCacheFixed = 8.0, kCacheStage = 2.8;
+// Workgroups of so many rounds of the chip are not cut further: parts take workspace.
+constexpr int64_t kManyRounds = 8;
 
 // Parts of caches of more than 32 packed rows, 4 stages at least, expected to end first:
 // rounds of the chip, two workgroups a CU, and the merge's us of a part.  us with the merge:
@@ -703,6 +705,7 @@ int tile_parts(int64_t groups, int64_t cap) {
   double best = 0.0;
   int parts = 1;
   for (int64_t p = 1; p <= std::max<int64_t>(1, std::min<int64_t>(stages / 4, places)); ++p) {
+    if (p > 1 && groups * p > kManyRounds * places) break;
     const double t = (groups * p + places - 1) / places *
                          (kCacheFixed + (stages + p - 1) / p * kCacheStage) +
                      kMergePart * groups * p;
@@ -732,6 +735,7 @@ void plan_prefix(int64_t rows, int64_t P, int Hkv, double caches, CachePlan* p) 
     const int64_t n = (rows * ks + 127) / 128 * Hkv;
     for (int64_t parts = 1; parts <= std::min<int64_t>(stages, 2 * kCUs); ++parts) {
       const int64_t w = n * parts, rest = w % (2 * kCUs), st = (stages + parts - 1) / parts;
+      if (parts > 1 && w > kManyRounds * 2 * kCUs) break;
       const double more = std::max(0.0, (double)(rest - kCUs) / kCUs);
       double t = w / (2 * kCUs) * (kCacheFixed + st * both) + kMergePart * (2.0 / ks) * w;
       if (rest > 0) t += kCacheFixed + st * (alone + more * (both - alone));

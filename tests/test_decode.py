@@ -266,3 +266,11 @@ def test_caches_of_very_different_lengths(nq, Hq, Hkv):
     torch.cuda.synchronize()
     _check(o, lse, _Ref(q, k, v, lens))
     assert torch.equal(o2[turn], o) and torch.equal(lse2[turn], lse)
+
+
+def test_large_calls_are_not_cut():
+    """Where whole tiles fill the chip many times a row has one part, or two with the prefix:
+    the workspace stays within a few times the rows."""
+    for B, nq, cap, P in ((65536, 1, 4096, 0), (4096, 8, 1 << 20, 1 << 20), (2000, 128, 65536, 999)):
+        size = upipe.upipe_attn_decode_workspace_size(B, nq, cap, P, 16, 4, D)
+        assert size - 16 == (1 + (P > 0)) * 129 * 4 * B * nq * 16, (B, nq, cap, P)
