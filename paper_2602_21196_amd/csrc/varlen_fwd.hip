@@ -148,12 +148,18 @@ __device__ __forceinline__ void fwd_stage(const char* smem, uint32_t k_at, uint3
 }
 
 // The KS parts of every row folded in fp32, in ascending key order: parts 1..
-// pass (m_ref, l, acc) through the stage buffers (16 KB per wave) with fold_out,
-// part 0 takes them with fold_in; a barrier before each.
-template <int KS>
+// pass (m_ref, l, acc) through the stage buffers (16 KB per wave, and behind all of these
+// 512 bytes per wave) with fold_out, part 0 takes them with fold_in; a barrier before each.
+template <int KS, int NW>
+struct Fold {
+  static constexpr int NQW = NW / KS;      // waves along the rows
+  static_assert((KS - 1) * NQW * (4096 + 128) * (int)sizeof(float) <= 2 * Stage<NW>::BYTES,
+                "the parts fit into the stage buffers");
+};
+template <int KS, int NW>
 __device__ __forceinline__ void fold_out(char* smem, int ks, int wq, int lane,
                                          const f32x16 (&oacc)[4], float m_ref, float l_tot) {
-  constexpr int NQW = 8 / KS;
+  constexpr int NQW = Fold<KS, NW>::NQW;
   float* fold = reinterpret_cast<float*>(smem);
   float* fold_ml = fold + (KS - 1) * NQW * 4096;
   const int slot = (ks - 1) * NQW + wq;
@@ -170,10 +176,10 @@ __device__ __forceinline__ void fold_out(char* smem, int ks, int wq, int lane,
   fold_ml[slot * 128 + 64 + lane] = l_tot;
 }
 
-template <int KS>
+template <int KS, int NW>
 __device__ __forceinline__ void fold_in(const char* smem, int wq, int lane, f32x16 (&oacc)[4],
                                         float& m_ref, float& l_tot) {
-  constexpr int NQW = 8 / KS;
+  constexpr int NQW = Fold<KS, NW>::NQW;
   const float* fold = reinterpret_cast<const float*>(smem);
   const float* fold_ml = fold + (KS - 1) * NQW * 4096;
 #pragma unroll
@@ -478,10 +484,10 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
   float l_tot = l_run + __shfl_xor(l_run, 32);
   if (KS > 1) {
     __syncthreads();   // every wave is done reading the last stage, and copying
-    if (ks > 0) fold_out<KS>(smem, ks, wq, lane, oacc, m_ref, l_tot);
+    if (ks > 0) fold_out<KS, NW>(smem, ks, wq, lane, oacc, m_ref, l_tot);
     __syncthreads();
     if (ks > 0) return;
-    fold_in<KS>(smem, wq, lane, oacc, m_ref, l_tot);
+    fold_in<KS, NW>(smem, wq, lane, oacc, m_ref, l_tot);
   }
   mend_row(row_ok, kp, a.k.row, vp, a.v.row, j0 * BKS, min(lim + 1, j1 * BKS), lim,
            min(it.Lk, min(j1, (seen_w + BKS - 1) / BKS) * BKS), qf, g, oacc, m_ref, l_tot);
