@@ -203,13 +203,16 @@ __device__ __forceinline__ void fold_in(const char* smem, int wq, int lane, f32x
 }
 
 // A row against its keys by plain arithmetic.  The lane pair of a row has its query and
-// output elements as the tile has them.  Ends early once a visible score is not a
-// number, or no element is finite any more: so it stays.
+// output elements as the tile has them.  Ends early once a visible score is not a number, or
+// no element of the output is one: so they stay (an infinite one may still meet its
+// opposite).  Then m_ref and l are the tile's again, all keys' sums, which no value enters;
+// with large_scores they are not to be had from there, and every key is taken.
 __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const bf16* v,
                                             int64_t v_row, int64_t key0, int64_t key1,
-                                            const bf16x8 (&qf)[8], int g, f32x16 (&oacc)[4],
-                                            float& m_ref, float& l) {
+                                            const bf16x8 (&qf)[8], int g, bool large_scores,
+                                            f32x16 (&oacc)[4], float& m_ref, float& l) {
   const float sl2 = 1.4426950408889634f * 0.08838834764831845f;
+  const float m_tile = m_ref, l_tile = l;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
@@ -242,12 +245,16 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
           oacc[dt][4 * a + b] = fmaf(p, (float)vv[b], oacc[dt][4 * a + b] * alpha);
       }
     if (!(l == l)) break;
-    float least = INFINITY;        // of the absolute values; NaN are passed over
+    bool some = large_scores;      // element that is a number
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) least = fminf(least, fabsf(oacc[dt][i]));
-    if (fminf(least, __shfl_xor(least, 32)) == INFINITY) break;
+      for (int i = 0; i < 16; ++i) some |= oacc[dt][i] == oacc[dt][i];
+    if (!(some | (bool)__shfl_xor((int)some, 32))) {
+      m_ref = m_tile;
+      l = l_tile;
+      break;
+    }
   }
 }
 
@@ -280,7 +287,7 @@ __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_r
     }
   }
   z += __shfl_xor(z, 32);
-  if (!(z == z)) careful_row(k, k_row, v, v_row, key0, key1, qf, g, oacc, m_ref, l);
+  if (!(z == z)) careful_row(k, k_row, v, v_row, key0, key1, qf, g, far, oacc, m_ref, l);
 }
 
 // A row's result, by the lane pair that holds it: the part's, in fp32, or the row's own.

@@ -1,0 +1,70 @@
+"""Values that are infinite or not a number, some visible and some masked, in the forward
+over packed sequences and over caches: what they may change and what they may not."""
+
+import pytest
+import torch
+
+import varlen_ref as R
+from paper_2602_21196_amd import upipe
+from test_varlen import _normal
+
+DEV = "cuda:0"
+D = 128
+pytestmark = pytest.mark.gpu
+
+VALUES = [float("nan"), float("inf")]
+BATCHES = [([300, 40], 4), ([300, 40], 1), ([2000, 9], 16)] + [([64 + i % 3 for i in range(70)], 32)]
+
+
+@pytest.mark.parametrize("bad", VALUES)
+@pytest.mark.parametrize("lens,Hq", BATCHES)
+def test_log_sum_exps_do_not_depend_on_values(bad, lens, Hq):
+    """A whole value row is bad where it is visible, and a later one of its stage where it
+    is masked: no element of the rows between them is finite, but their lse is
+    that of all their keys, and with it dV, which no value enters."""
+    cu = [sum(lens[:i]) for i in range(len(lens) + 1)]
+    q, k, v, dout = (_normal((cu[-1], H, D), j) for j, H in enumerate((Hq, 1, 1, Hq)))
+    plan = upipe.VarlenPlan(cu, Hq=Hq, Hkv=1, device=DEV)
+    ref = R.Packed(q, k, v, cu, cu, True, dout)
+    for first, second in ((10, 50), (0, 31), (5, 63)):
+        bv = v.clone()
+        bv[[first, second]] = bad
+        o, lse = upipe.attn_fwd_varlen(q, k, bv, plan)
+        _, _, dv = upipe.attn_bwd_varlen(q, k, bv, o, lse, dout, plan)
+        torch.cuda.synchronize()
+        R.check("lse", lse, ref.lse,
+                R.score_error(ref.s_lse) + 4 * R.FP32 * ref.lse.abs() + 8 * R.FP32)
+        assert not bool(o[first:lens[0]].isfinite().any())
+        clean = torch.cat([o[:first], o[lens[0]:]])
+        assert bool(clean.isfinite().all())
+        es = float(R.score_error(ref.s_lse.max()))
+        c = R.BF16 + (1 + R.BF16) * (3 * es + 16 * R.FP32)
+        R.check("dv", dv, ref.dv, R.BF16 * ref.dv.abs() + (1 + R.BF16) * c * ref.a_dv + 1e-30)
+
+
+def test_opposite_infinities_are_not_a_number():
+    """Row i sees +inf at key 10 and, from row 20 on, -inf at key 20; key 50's NaN is
+    masked for the rows before it."""
+    n = 64
+    q, k, v = _normal((n, 2, D), 1), _normal((n, 1, D), 2), _normal((n, 1, D), 3)
+    v[10], v[20], v[50] = float("inf"), float("-inf"), float("nan")
+    o, lse = upipe.attn_fwd_varlen(q, k, v, upipe.VarlenPlan([0, n], Hq=2, Hkv=1, device=DEV))
+    torch.cuda.synchronize()
+    assert bool(o[:10].isfinite().all()) and bool((o[10:20] == float("inf")).all())
+    assert bool(o[20:].isnan().all()) and bool(lse.isfinite().all())
+
+
+@pytest.mark.parametrize("bad", VALUES)
+def test_large_scores_beside_bad_values(bad):
+    """Scores beyond 2^30 and a bad visible value: lse is that of all keys."""
+    n = 100
+    q = torch.full((n, 1, D), 1e8, dtype=torch.bfloat16, device=DEV)
+    k = torch.full((n, 1, D), -1e3, dtype=torch.bfloat16, device=DEV)
+    v = _normal((n, 1, D), 3)
+    v[[3, 70]] = bad
+    o, lse = upipe.attn_fwd_varlen(q, k, v, upipe.VarlenPlan([0, n], Hq=1, Hkv=1, device=DEV))
+    score = float((q[0, 0].double() * k[0, 0].double()).sum()) / D ** 0.5
+    torch.cuda.synchronize()
+    R.check("lse", lse, torch.full_like(lse, score, dtype=torch.float64),
+            torch.full_like(lse, (D + 8) * R.FP32 * abs(score), dtype=torch.float64))
+    assert bool(o[:3].isfinite().all()) and not bool(o[3:].isfinite().any())
