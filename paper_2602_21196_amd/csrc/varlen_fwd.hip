@@ -524,7 +524,9 @@ __global__ __launch_bounds__(256, 2) void rows_prefix_kernel(RowFwdArgs p, RowFw
 // The parts of every row to o and lse: weights e^(lse_i - max), the sums in fp32, one
 // rounding.  Sixteen lanes a row, GP groups of them to share many parts: first the
 // weights of all parts, then their outputs, several loads under way at a time (one
-// after the other 256 parts of 8 rows took 17 us, twice what forming them did).
+// after the other 256 parts of 8 rows took 17 us, twice what forming them did).  An empty
+// part has the weight -1: its row is not written, where a part whose weight is 0 in fp32
+// may hold a visible value that is infinite or not a number.
 template <int GP, bool PLANNED>
 __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
   constexpr int ROWS = 16 / GP;                       // of a workgroup
@@ -559,9 +561,9 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
     // (a NaN is passed over by fmaxf and comes in with its weight)
 #pragma unroll
     for (int u = 0; u < kSomeParts / 16; ++u) {
-      const float wt = v[u] == -INFINITY ? 0.f : v[u] == m ? 1.f : __expf(v[u] - m);
+      const float wt = v[u] == -INFINITY ? -1.f : v[u] == m ? 1.f : __expf(v[u] - m);
       weights[lr][c + 16 * u] = wt;
-      l += wt;
+      l += wt < 0.f ? 0.f : wt;
     }
 #pragma unroll
     for (int off = 8; off >= 1; off >>= 1) l += __shfl_xor(l, off);
@@ -579,9 +581,9 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
     m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     for (int i = threadIdx.x; i < parts; i += 256) {
       const float v = weights[0][i];
-      const float wt = v == -INFINITY ? 0.f : v == m ? 1.f : __expf(v - m);
+      const float wt = v == -INFINITY ? -1.f : v == m ? 1.f : __expf(v - m);
       weights[0][i] = wt;
-      l += wt;
+      l += wt < 0.f ? 0.f : wt;
     }
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) l += __shfl_xor(l, off);
@@ -603,11 +605,11 @@ __global__ __launch_bounds__(256) void rows_merge_kernel(RowMergeArgs a) {
       const float* p = po + i * rows * HEAD_DIM;
       lo[u] = *reinterpret_cast<const f32x4*>(p);
       hi[u] = *reinterpret_cast<const f32x4*>(p + 4);
-      wt[u] = i0 + u * GP < parts ? weights[lr][i] : 0.f;
+      wt[u] = i0 + u * GP < parts ? weights[lr][i] : -1.f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool empty = wt[u] == 0.f;       // an empty part's row is not written
+      const bool empty = wt[u] < 0.f;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         acc[e] = fmaf(wt[u], empty ? 0.f : lo[u][e], acc[e]);

@@ -68,3 +68,34 @@ def test_large_scores_beside_bad_values(bad):
     R.check("lse", lse, torch.full_like(lse, score, dtype=torch.float64),
             torch.full_like(lse, (D + 8) * R.FP32 * abs(score), dtype=torch.float64))
     assert bool(o[:3].isfinite().all()) and not bool(o[3:].isfinite().any())
+
+
+@pytest.mark.parametrize("bad", VALUES)
+@pytest.mark.parametrize("at", [0, 700, 4999])
+def test_a_visible_value_reaches_the_row_from_every_part(bad, at):
+    """Key 5000 has a score 220 above the others', so the weights of parts without it are 0
+    in fp32 (e^-220 = 2^-317): a bad value there is visible all the same.  In parts of a
+    cache, in parts of a packed sequence, behind a prefix, and whole."""
+    n, Hq = 20000, 8
+    q = torch.ones((4, Hq, D), dtype=torch.bfloat16, device=DEV)
+    k = torch.zeros((n, 1, D), dtype=torch.bfloat16, device=DEV)
+    v = _normal((n, 1, D), 3)
+    k[5000] = 220 / D ** 0.5                    # 128 products over sqrt 128
+    v[at, 0, 3] = bad
+    score = float(k[5000, 0].double().sum()) / D ** 0.5
+    lens = torch.tensor([n], dtype=torch.int32, device=DEV)
+    plan = upipe.VarlenPlan([0, 4], [0, n], Hq=Hq, Hkv=1, device=DEV)
+    assert plan.fwd_workspace > 4096            # keys in parts
+    runs = {"cache": upipe.attn_decode(q[None], k[None], v[None], lens),
+            "prefix": upipe.attn_decode(q[None], k[None, 6000:], v[None, 6000:], lens - 6000,
+                                        k[:6000], v[:6000]),
+            "packed": upipe.attn_fwd_varlen(q, k, v, plan)}
+    torch.cuda.synchronize()
+    for name, (o, lse) in runs.items():
+        o = o.reshape(4 * Hq, D)
+        rest = [e for e in range(D) if e != 3]
+        print(f"  {name}: {int((~o[:, 3].isfinite()).sum())} of {4 * Hq} rows", flush=True)
+        assert not bool(o[:, 3].isfinite().any()), name
+        assert bool(o[:, rest].isfinite().all()), name
+        R.check("lse", lse, torch.full_like(lse, score, dtype=torch.float64),
+                torch.full_like(lse, (D + 8) * R.FP32 * score, dtype=torch.float64))
