@@ -283,10 +283,12 @@ __global__ __launch_bounds__(1024) void norm_dw_fold_kernel(const float* __restr
 }  // namespace
 
 // Workgroups of one tensor's rows: every lane group has one pair of heads while that
-// needs no more than `most` workgroups.
+// needs no more than `most` workgroups, and 2048 pairs at most: dw's fp32 sums are of up
+// to 4096 rows each, whose rounding stays below 2^-12 of their terms.
 static int norm_blocks(int64_t T, int H, int most) {
   const int64_t n = (T * ((H + 1) / 2) + kPairsPerBlock - 1) / kPairsPerBlock;
-  return (int)(n < most ? n : most);
+  const int64_t least = (n + 2047) / 2048;
+  return (int)(n < most ? n : least > most ? least : most);
 }
 
 constexpr int kNormFwdBlocks = 4096, kNormBwdBlocks = 1024;
