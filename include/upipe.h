@@ -275,7 +275,10 @@ int upipe_rope(void* x, int64_t S, int H, int d, int64_t pos0, double base, int 
  * multiples of 8, p 16-byte aligned.  Q, K and V may so be columns of one
  * projection's output; a dense [T, H, d] has row = H d, head = d.  Rows that a call
  * writes must not share elements with each other or with rows that it reads,
- * other than as a call allows (UPIPE_ERR_INVALID_ARG).
+ * other than as a call allows (UPIPE_ERR_INVALID_ARG).  Two tensors are known to be
+ * apart where their ranges are, where both lie side by side in every row or every head of
+ * one buffer, or where all strides are multiples of one in which their rows of d
+ * lie beside each other; other layouts are taken to share.
  * ---------------------------------------------------------------------- */
 typedef struct {
   void* p;
@@ -342,7 +345,8 @@ int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
  * Attention of a few new tokens of every sequence against its cache, and against
  * a prefix that all sequences share.
  *
- *   q, o   rows [B nq, Hq, d]: token t of sequence b is row b nq + t; o may be q
+ *   q, o   rows [B nq, Hq, d]: token t of sequence b is row b nq + t; o may be q; o
+ *          lies outside what the caches span
  *   k, v   rows [cap, Hkv, d] of cache 0; cache b lies b * k_cache (v_cache)
  *          elements on
  *   lens   int32 [B] on the DEVICE: valid rows of each cache, the nq new ones

@@ -126,17 +126,27 @@ bool heads_apart(const upipe_heads& a, int64_t Ta, int Ha, const upipe_heads& b,
   if (Ta < 1 || Tb < 1) return true;
   if (!overlap(a.p, 2 * heads_span(a, Ta, Ha), b.p, 2 * heads_span(b, Tb, Hb))) return true;
   const int64_t d = ((int64_t)(uintptr_t)b.p - (int64_t)(uintptr_t)a.p) / 2;
-  if (a.row == b.row && a.row > 0) {
-    const int64_t sa = (Ha - 1) * a.head + HEAD_DIM, sb = (Hb - 1) * b.head + HEAD_DIM;
-    const int64_t at = ((d % a.row) + a.row) % a.row;
-    if (sa <= at && at + sb <= a.row) return true;
-  }
-  const int64_t h = a.head;
-  if (h == b.head && h >= 2 * HEAD_DIM && a.row % h == 0 && b.row % h == 0) {
-    const int64_t at = ((d % h) + h) % h;
-    if (at >= HEAD_DIM && at + HEAD_DIM <= h) return true;
-  }
-  return false;
+  // All that a row of a spans, in every `step` elements, before or behind all of b's.
+  auto side_by_side = [&](int64_t step, int64_t span_a, int64_t span_b) {
+    const int64_t at = ((d % step) + step) % step;
+    return span_a <= at && at + span_b <= step;
+  };
+  if (a.row == b.row && a.row > 0 &&
+      side_by_side(a.row, (Ha - 1) * a.head + HEAD_DIM, (Hb - 1) * b.head + HEAD_DIM))
+    return true;
+  if (a.head == b.head && a.head > 0 &&
+      side_by_side(a.head, (Ta - 1) * a.row + HEAD_DIM, (Tb - 1) * b.row + HEAD_DIM))
+    return true;
+  // Single rows on a common grid: every stride a multiple of the smallest.
+  const int64_t strides[4] = {Ta > 1 ? a.row : 0, Ha > 1 ? a.head : 0, Tb > 1 ? b.row : 0,
+                              Hb > 1 ? b.head : 0};
+  int64_t grid = 0;
+  for (int64_t s : strides)
+    if (s > 0 && (grid == 0 || s < grid)) grid = s;
+  if (grid == 0) return false;
+  for (int64_t s : strides)
+    if (s % grid != 0) return false;
+  return side_by_side(grid, HEAD_DIM, HEAD_DIM);
 }
 
 // ----------------------------------------------------------- ws planning

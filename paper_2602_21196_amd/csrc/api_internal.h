@@ -84,7 +84,8 @@ bool heads_ok(const upipe_heads& v, int64_t T, int H);
 // No two of the T x H rows share an element.
 bool heads_distinct(const upipe_heads& v, int64_t T, int H);
 // No row of a shares an element with one of b, as far as that shows: disjoint
-// ranges, columns of one row, or places of one head (K beside V in each).
+// ranges, columns of one row (or of one head's rows), or rows between each other (K beside
+// V in each head).
 bool heads_apart(const upipe_heads& a, int64_t Ta, int Ha, const upipe_heads& b, int64_t Tb, int Hb);
 inline bool heads_same(const upipe_heads& a, const upipe_heads& b) {
   return a.p == b.p && a.row == b.row && a.head == b.head;
