@@ -99,3 +99,49 @@ def test_a_visible_value_reaches_the_row_from_every_part(bad, at):
         assert bool(o[:, rest].isfinite().all()), name
         R.check("lse", lse, torch.full_like(lse, score, dtype=torch.float64),
                 torch.full_like(lse, (D + 8) * R.FP32 * score, dtype=torch.float64))
+
+
+REACH = 192          # of a masked pair's bad row in the backward, in keys
+
+
+@pytest.mark.parametrize("Lq,Lk,G", [(512, 513, 1), (512, 639, 1), (400, 400, 3), (700, 1000, 2),
+                                     (300, 290, 5), (256, 256, 16)])
+def test_how_far_a_masked_pair_reaches_in_the_backward(Lq, Lk, G):
+    """Gradients of rows and keys from 192 on behind a bad row's last visible key keep their
+    bits: a tile of 128 rows and a block of 128 keys meet with 127 keys and half a tile between
+    a row's last key and a key, a stage of keys and the 32 rows of a wave with less."""
+    q, dout = _normal((Lq, G, D), 1), _normal((Lq, G, D), 2)
+    k, v = _normal((Lk, 1, D), 3), _normal((Lk, 1, D), 4)
+    plan = upipe.VarlenPlan([0, Lq], [0, Lk], Hq=G, Hkv=1, device=DEV)
+    o, lse = upipe.attn_fwd_varlen(q, k, v, plan)
+    want = upipe.attn_bwd_varlen(q, k, v, o, lse, dout, plan)
+    far = 0
+    for i in (0, 1, 63, 64, 127, 128, 191, Lq - 1):
+        if i >= Lq:
+            continue
+        last = i + Lk - Lq                  # the bad row's last key
+        for bad in VALUES:
+            for at in (0, 1):
+                x = [q.clone(), dout.clone()]
+                x[at][i] = bad
+                got = upipe.attn_bwd_varlen(x[0], k, v, o, lse, x[1], plan)
+                torch.cuda.synchronize()
+                for a, b in zip(got[1:], want[1:]):
+                    other = (a != b).any(-1).any(-1).nonzero()
+                    far = max(far, int(other.max()) - last if other.numel() else 0)
+                keep = torch.arange(Lq, device=DEV) != i
+                assert torch.equal(got[0][keep], want[0][keep])
+    near = 0
+    for j in (0, 5, 127, 128, 255, Lk - 1):
+        if j >= Lk:
+            continue
+        for bad in VALUES:
+            bk = k.clone()
+            bk[j] = bad
+            got = upipe.attn_bwd_varlen(q, bk, v, o, lse, dout, plan)
+            torch.cuda.synchronize()
+            other = (got[0] != want[0]).any(-1).any(-1).nonzero()
+            near = max(near, j - (int(other.min()) + Lk - Lq) if other.numel() else 0)
+    print(f"  a row reaches {far} keys behind its last, a key {near} rows before its first",
+          flush=True)
+    assert far < REACH and near < REACH
