@@ -28,8 +28,8 @@ if ROOT not in sys.path:
 METRIC = ("attention fwd+bwd TFLOP/s (causal) per MI355X; "
           "peak activation GB vs chunk size U")
 KERNEL_SOURCES = {"attn_fwd": ("attn_fwd.hip", "common.h"),
-                  "attn_bwd_dkdv": ("attn_bwd.hip", "common.h"),
-                  "attn_bwd_dq": ("attn_bwd.hip", "common.h")}
+                  "attn_bwd_dkdv": ("attn_bwd.hip", "attn_bwd_tile.h", "common.h"),
+                  "attn_bwd_dq": ("attn_bwd.hip", "attn_bwd_tile.h", "common.h")}
 PEAK_BF16_TFLOPS = 2516.6   # 256 CU x 4096 flop/clk x 2.4 GHz, dense bf16
 PEAK_HBM_GBS = 8000.0
 
