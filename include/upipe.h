@@ -311,8 +311,10 @@ typedef struct {
  *   lse    fp32, head h of query row t at lse[h * lse_head + t]
  * Scores, softmax and sums are fp32; the weights are rounded to bf16 for their product
  * with v.  lse carries no rounding to bf16.  A masked value that is infinite or
- * not a number does not reach a row; a visible one does.  The results depend on the
- * lengths and head counts of the whole plan in their last bits.
+ * not a number does not reach a row; a visible one does.  Rows before such a value in its
+ * stage of keys, and rows of scores beyond 2^30, are formed again key by key, which takes
+ * some 60 times as long as the others.  The results depend on the lengths and head counts
+ * of the whole plan in their last bits.
  * ---------------------------------------------------------------------- */
 size_t upipe_varlen_plan_size(const int64_t* cu_q, const int64_t* cu_k, int n_seq, int Hq, int Hkv,
                               int d, int causal);

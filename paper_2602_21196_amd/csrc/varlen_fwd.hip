@@ -258,15 +258,85 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
   }
 }
 
+// Infinite or not a number.
+__device__ __forceinline__ bool odd(float x) { return !(fabsf(x) < INFINITY); }
+
+// The odd elements of the wave's rows: what the odd visible values of their column add up
+// to, +-inf or not a number; that is the result, whatever the weights and the finite values.
+// The wave goes through the keys that all of its rows see, key0 .. common - 1, two columns
+// a lane, a row through its rest, to key1.  Returns whether an element is left whose visible
+// values are all finite, which it looks for in rows with `mine`.
+__device__ __forceinline__ int settle_columns(const bf16* v, int64_t v_row, int key0, int common,
+                                              int key1, bool mine, f32x16 (&oacc)[4]) {
+  const int lane = threadIdx.x & 63, g = lane >> 5;
+  float sum[2] = {0.f, 0.f};
+  const bf16* p = v + key0 * v_row + 2 * lane;
+  auto take = [&](uint32_t x) {
+    const float lo = __uint_as_float(x << 16), hi = __uint_as_float(x & 0xffff0000u);
+    sum[0] += odd(lo) ? lo : 0.f;
+    sum[1] += odd(hi) ? hi : 0.f;
+  };
+  constexpr int U = 8;      // loads under way
+  const int rest = max(common, key0);
+  int j0 = key0;
+  for (; j0 + U <= common; j0 += U) {
+    uint32_t x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u, p += v_row) x[u] = *reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+    for (int u = 0; u < U; ++u) take(x[u]);
+    if (__builtin_amdgcn_ballot_w64(sum[0] == sum[0] || sum[1] == sum[1]) == 0) common = j0;
+  }
+#pragma unroll 1
+  for (; j0 < common; ++j0, p += v_row) take(*reinterpret_cast<const uint32_t*>(p));
+  constexpr float OPEN = 3.4028235e38f;      // an odd element whose visible values are not, so far
+  const float open = mine ? OPEN : NAN;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      // of column 32 dt + 8 (i / 4) + 4 g + i % 4
+      const float c = __shfl(sum[i & 1], 16 * dt + 4 * (i >> 2) + 2 * g + ((i & 3) >> 1));
+      oacc[dt][i] = odd(oacc[dt][i]) ? odd(c) ? c : open : oacc[dt][i];
+      // (a condition is a pair of scalar registers: those of 64 elements would spill)
+      if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll 1
+  for (int j = rest; j < key1; ++j) {
+    const bf16* vp = v + j * v_row + 4 * g;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const bf16x4 x = *reinterpret_cast<const bf16x4*>(vp + 32 * dt + 8 * a);
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          const float o = oacc[dt][4 * a + b], y = (float)x[b];
+          oacc[dt][4 * a + b] = odd(y) ? o == OPEN ? y : o + y : o;
+        }
+        if (a % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
+  }
+  float least = 1.f;
+#pragma unroll
+  for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) least = fminf(least, fabsf(oacc[dt][i] - OPEN));
+  return least == 0.f;
+}
+
 // A masked key's weight is 0, but the matrix instructions also multiply that 0 by the
 // key's value, which may be infinite or not a number: then the rows of its stage come
-// out as NaN.  Such a row is formed again without it.  `lim`: the row's last key, `end`:
-// the end of the keys that its tile multiplied.  So is a row of scores beyond 2^30:
-// there the rounding of their maximum, which the stages' fused multiply-adds see, is
-// more than exp2 spans.
+// out as NaN.  Where a row's visible values are odd in the same columns that settles it;
+// else it is formed again without the masked ones.  (All rows again, where one column of every
+// value is odd: 32768 tokens of 8 heads 123 ms, settled 5.3, clean 2.0.)  `lim`: the row's
+// last key, lim_w: the first row's of the wave, key1: the end of the row's keys of this part,
+// `end`: the end of the keys that its tile multiplied.  So is a row of scores beyond 2^30
+// formed again: there the rounding of their maximum, which the stages' fused multiply-adds
+// see, is more than exp2 spans.
 __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_row, const bf16* v,
-                                         int64_t v_row, int key0, int key1, int lim, int end,
-                                         const bf16x8 (&qf)[8], int g, f32x16 (&oacc)[4],
+                                         int64_t v_row, int key0, int key1, int lim, int lim_w,
+                                         int end, const bf16x8 (&qf)[8], int g, f32x16 (&oacc)[4],
                                          float& m_ref, float& l) {
   float z = 0.f;
 #pragma unroll
@@ -275,9 +345,11 @@ __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_r
     for (int i = 0; i < 16; ++i) z = fmaf(oacc[dt][i], 0.f, z);
   z += __shfl_xor(z, 32);
   const bool far = m_ref != kNoMax && fabsf(m_ref) > 1073741824.f;
-  if (!row_ok || (z == z && !far)) return;      // both lanes of a row alike
-  z = far ? NAN : 0.f;
-  for (int j = max(lim + 1, key0); j < end && !far; ++j) {
+  const bool bad = row_ok && (far || !(z == z));      // both lanes of a row alike
+  if (__builtin_amdgcn_ballot_w64(bad) == 0) return;
+  bool again = bad && far, mine = bad && !far;
+  z = 0.f;
+  for (int j = max(lim + 1, key0); j < end && mine; ++j) {
     const bf16* p = v + j * v_row + 64 * g;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -287,7 +359,12 @@ __device__ __forceinline__ void mend_row(bool row_ok, const bf16* k, int64_t k_r
     }
   }
   z += __shfl_xor(z, 32);
-  if (!(z == z)) careful_row(k, k_row, v, v_row, key0, key1, qf, g, far, oacc, m_ref, l);
+  mine = mine && !(z == z);      // a masked value is to blame
+  if (__builtin_amdgcn_ballot_w64(mine) != 0) {
+    const int left = settle_columns(v, v_row, key0, min(lim_w + 1, end), key1, mine, oacc);
+    again |= (left | __shfl_xor(left, 32)) != 0;
+  }
+  if (again) careful_row(k, k_row, v, v_row, key0, key1, qf, g, far, oacc, m_ref, l);
 }
 
 // A row's result, by the lane pair that holds it: the part's, in fp32, or the row's own.
@@ -497,7 +574,7 @@ __device__ __forceinline__ void rows_fwd(const RowFwdArgs& a, char* smem, int bl
     fold_in<KS, NW>(smem, wq, lane, oacc, m_ref, l_tot);
   }
   mend_row(row_ok, kp, a.k.row, vp, a.v.row, j0 * BKS, min(lim + 1, j1 * BKS), lim,
-           min(it.Lk, min(j1, (seen_w + BKS - 1) / BKS) * BKS), qf, g, oacc, m_ref, l_tot);
+           lim_w, min(it.Lk, min(j1, (seen_w + BKS - 1) / BKS) * BKS), qf, g, oacc, m_ref, l_tot);
   if (!row_ok) return;
   const bool part =
       MODE == kRowsOne || (MODE == kRowsCache ? a.splits + a.part0 : it.parts) > 1;

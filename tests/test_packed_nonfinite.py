@@ -145,3 +145,63 @@ def test_how_far_a_masked_pair_reaches_in_the_backward(Lq, Lk, G):
     print(f"  a row reaches {far} keys behind its last, a key {near} rows before its first",
           flush=True)
     assert far < REACH and near < REACH
+
+
+@pytest.mark.parametrize("bad", [*VALUES, "mixed"])
+@pytest.mark.parametrize("lens,Hq,part", [([9000], 4, False), ([4, 300], 8, True), ([700, 33, 1], 2, False)])
+def test_a_bad_column_of_every_value(bad, lens, Hq, part):
+    """A column that is bad in every row: bad in every result, the others what they are.  With
+    infinities of both signs a row has that of its only key, or no number."""
+    lk = [20000, 300] if part else lens
+    cu_q, cu_k = ([sum(x[:i]) for i in range(len(x) + 1)] for x in (lens, lk))
+    q, k, v = (_normal((n, H, D), j) for j, (n, H) in enumerate(
+        ((cu_q[-1], Hq), (cu_k[-1], 1), (cu_k[-1], 1))))
+    plan = upipe.VarlenPlan(cu_q, cu_k, Hq=Hq, Hkv=1, device=DEV)
+    ref = R.Packed(q, k, v, cu_q, cu_k, True)
+    bv = v.clone()
+    inf = float("inf")
+    for col in (0, 37, 127):
+        bv[:, 0, col] = inf if bad == "mixed" else bad
+    if bad == "mixed":
+        bv[1::2, 0, 37] = -inf
+    o, lse = upipe.attn_fwd_varlen(q, k, bv, plan)
+    torch.cuda.synchronize()
+    R.check("lse", lse, ref.lse,
+            R.score_error(ref.s_lse) + 4 * R.FP32 * ref.lse.abs() + 8 * R.FP32)
+    if bad == "mixed":
+        assert bool((o[:, :, [0, 127]] == inf).all())
+        first = torch.zeros(cu_q[-1], dtype=torch.bool, device=DEV)       # rows of one key
+        first[[a for a, x, y in zip(cu_q, lens, lk) if x == y]] = True
+        assert bool(o[~first][:, :, 37].isnan().all()) and bool(o[first][:, :, 37].isinf().all())
+    else:
+        want = o.isnan() if bad != bad else o == inf
+        assert bool(want[:, :, [0, 37, 127]].all())
+    keep = [e for e in range(D) if e not in (0, 37, 127)]
+    es = R.score_error(ref.s_lse)
+    w = R.BF16 + 2 * es.T[..., None] + 8 * R.FP32
+    R.check("others", o[:, :, keep], ref.o[:, :, keep],
+            (R.BF16 * ref.o.abs() + (1 + R.BF16) * w * ref.a_o)[:, :, keep] + 1e-30)
+
+
+@pytest.mark.parametrize("bad", VALUES)
+def test_a_bad_column_takes_no_lifetime(bad):
+    """One bad column of every value in a long sequence, as a diverged step leaves it: no
+    more than 30 times as long as clean ones (formed again key by key it was 62)."""
+    n = 16384
+    q, k, v = _normal((n, 8, D), 1), _normal((n, 1, D), 2), _normal((n, 1, D), 3)
+    plan = upipe.VarlenPlan([0, n], Hq=8, Hkv=1, device=DEV)
+    times = []
+    for spoil in (False, True):
+        if spoil:
+            v[:, 0, 5] = bad
+        upipe.attn_fwd_varlen(q, k, v, plan)
+        torch.cuda.synchronize()
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        for _ in range(3):
+            upipe.attn_fwd_varlen(q, k, v, plan)
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b) / 3)
+    print(f"  clean {times[0]:.3f} ms, with a bad column {times[1]:.3f}", flush=True)
+    assert times[1] <= 30 * times[0]
