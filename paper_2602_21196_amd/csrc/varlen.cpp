@@ -102,9 +102,10 @@ struct Shape {
   double stage, fixed, full;
 };
 // What they lead to, us with 1 | 2 | 4 | half (* the chosen one): 16 documents of 256 tokens,
-// 32 heads on 8, 52 | 51 | 71 | 36*; 100 of up to 700, 8 on 1, 87 | 109 | 166 | 73*; 8
-// of 2048, 8 on 1, 80* | 93 | 136 | 82; 8192 tokens, 4 on 1, 172 | 106 | 93* | 137; 32768
-// tokens, 4 on 1, 903* | 978 | 1182 | 1022; 512 tokens, 4 on 1, 22 | 16 | 14* | 17.
+// 32 heads on 8, 51 | 51 | 73 | 40*; 100 of up to 700, 8 on 1, 90 | 116 | 182 | 80*; 8
+// of 2048, 8 on 1, 78* | 92 | 131 | 78; 8192 tokens, 4 on 1, 91 (its keys in parts, merged) |
+// 104 | 89* | 136; 32768 tokens, 4 on 1, 903* | 976 | 1173 | 1015; 512 tokens, 4 on 1, 22 |
+// 16 | 14* | 16.
 constexpr Shape kFwdShapes[4] = {{1, false, 128, 1, 3.5, 3.0, 10.0},
                                  {2, false, 128, 1, 2.0, 3.0, 7.0},
                                  {4, false, 128, 1, 1.2, 3.0, 6.5},
@@ -276,9 +277,9 @@ int choose_segment(const std::vector<Lengths>& seqs, int G, int Hkv, int causal)
   return best;
 }
 
-// Of dQ, as the forward's: 58* in halves against 76 (1) for 16 documents of 256 tokens, 109*
-// and 124 for 100 of up to 700, 116 and 111* for 8 of 2048; 8192 tokens, 4 heads on 1, 250 |
-// 144 | 114* | 184; 512 tokens 28 | 21 | 18* | 21.
+// Of dQ, as the forward's: 59* in halves against 66 (1) for 16 documents of 256 tokens, 118*
+// and 124 for 100 of up to 700, 111 and 109* for 8 of 2048; 8192 tokens, 4 heads on 1, 240 |
+// 141 | 111* | 183; 512 tokens 28 | 21 | 17* | 21.
 constexpr Shape kDqShapes[4] = {{1, false, 64, 1, 2.5, 4.0, 16.0},
                                 {2, false, 128, 1, 2.8, 4.0, 11.0},
                                 {4, false, 128, 1, 1.6, 4.0, 9.0},
@@ -752,13 +753,12 @@ void plan_prefix(int64_t rows, int64_t P, int Hkv, double caches, CachePlan* p) 
 // Parts of caches of up to 32 packed rows, which wait for memory alone: of 1024 rows, unless
 // they are more than four a CU, or of 2048, unless they are more than sixteen; or up to
 // twice as many (512 rows each at least) where that fills the chip, two workgroups a
-// CU, or whole rounds of it, better.  us with the
-// merge: 24 caches of 8192 rows, 8 heads, in 5 | 6 | 8 parts 153 | 172 | 156, of 1 to 16384
-// in 4 | 6 | 8 | 12 122 | 119 | 116 | 119; 64 of 1 to 16384 in 2 | 4 | 8 | 16 172 | 148 |
-// 139 | 154, 8 in 4 | 8 | 16 | 32 62 | 40 | 32 | 38; 40 of 8000, 2 heads, in 4 | 6 | 8 |
-// 12 80 | 69 | 83 | 72; 8 of 131000, one head, in 32 | 64 | 128 | 256 107 | 105 | 108 |
-// 113; one of 131072, parts of 256 | 512 | 1024 rows 48 | 37 | 33 before the merge had its
-// loads under way together, 23 with 512.
+// CU, or whole rounds of it, better.  us with the merge (* the chosen one; the best is within
+// 8 %): 24 caches of 8192 rows, 8 heads, in 2 | 5 | 6 | 8* | 16 parts 167 | 153 | 167 | 158 |
+// 163, of 1 to 16384 in 4 | 6 | 8* | 12 | 16 121 | 107 | 105 | 110 | 115; 64 of 1 to 16384 in
+// 2 | 4 | 8* | 16 414 | 393 | 394 | 406, 8 in 4 | 8 | 16* | 32 73 | 59 | 59 | 63; 40 of
+// 8000, 2 heads, in 4 | 6 | 8 | 12* 67 | 60 | 76 | 65; 8 of 131000, one head, in 32 | 64 |
+// 128* | 256 101 | 99 | 103 | 111; one of 131072 in 64 | 128 | 256* | 512 34 | 24 | 22 | 24.
 int few_parts(int64_t groups, int64_t cap) {
   const int64_t slots = 2 * kCUs;
   const int64_t most = std::min((cap + 511) / 512, kMostParts - slots);     // and a prefix's

@@ -18,8 +18,8 @@
 // behind it share a launch, so that the products of the one hide the other's loads.
 // What bounds it: MFMA issue where tiles fill the chip (131072 tokens, 4 heads on 1: 14.2
 // ms, 1240 TFLOP/s, as the forward over equal lengths; 65536 tokens in documents of up to
-// 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 100 us,
-// 5.1 TB/s, 24 of 8192 5.4; a plain read of as much 5.4), launches and one chain of
+// 32768, 8 heads: 2.29 ms, 1200), HBM in caches (24 of 1 to 16384 rows, 8 heads: 97 - 100
+// us, 5.1 - 5.3 TB/s, as 24 of 8192; a plain read of as much 5.4), launches and one chain of
 // stages in short calls.
 #include "varlen.h"
 
