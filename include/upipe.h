@@ -303,7 +303,8 @@ typedef struct {
  * call only, `plan_dev` by the kernels, which it has to outlive.  A plan serves any
  * number of calls, on any stream, also at once; a captured call keeps the list of work
  * that it was captured with, and reads `plan_dev` at every replay.  Hkv | Hq <= 64, d = 128,
- * up to 2^20 sequences of lengths up to 2^24 - 128.
+ * up to 2^20 sequences of lengths up to 2^24 - 128, of fewer than 2^23 tiles in all: 64 to
+ * 256 rows (query tokens times Hq / Hkv) of one sequence and key/value head.
  *
  *   q, o   rows [.., Hq, d], k, v rows [.., Hkv, d], up to the last offset at least;
  *          rows behind it are neither read nor written.  Rows of k and v are at
@@ -362,8 +363,9 @@ int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
  * read for all sequences together, and its weights join the cache's by
  * log-sum-exps in fp32.  How rows are split follows from B, nq, cap, P and the head counts,
  * never from lens, so a captured call may be replayed as the caches grow.  nq <= 128,
- * B <= 65536, cap and P up to 2^24 - 128, rows of k, v and the prefix at most 2^22
- * elements apart.  Numerics as above.
+ * B <= 65536, B nq Hq < 2^23 (with a prefix 2^22 - 4096), cap and P up to 2^24 - 128, rows
+ * of k, v and the prefix at most 2^22 elements apart (UPIPE_ERR_UNSUPPORTED).  Numerics as
+ * above.
  * ---------------------------------------------------------------------- */
 size_t upipe_attn_decode_workspace_size(int64_t B, int nq, int64_t cap, int64_t P, int Hq, int Hkv,
                                         int d);
