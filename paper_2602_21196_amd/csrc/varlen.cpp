@@ -332,14 +332,19 @@ int check_lengths(const int64_t* cu_q, const int64_t* cu_k, int n, int Hq, int H
   if (d != HEAD_DIM || Hq > kMaxHeads || n > kMaxSequences) return UPIPE_ERR_UNSUPPORTED;
   if (cu_q[0] != 0 || cu_k[0] != 0) return UPIPE_ERR_INVALID_ARG;
   seqs->resize(n);
+  int64_t tiles = 0, keys = 0;      // the least that the forward and dK/dV launch
   for (int i = 0; i < n; ++i) {
     if (cu_q[i + 1] < cu_q[i] || cu_k[i + 1] < cu_k[i]) return UPIPE_ERR_INVALID_ARG;
     const int64_t Lq = cu_q[i + 1] - cu_q[i], Lk = cu_k[i + 1] - cu_k[i];
     if (Lq > kMaxSeq || Lk > kMaxSeq || cu_q[i + 1] >= kMaxTokens || cu_k[i + 1] >= kMaxTokens)
       return UPIPE_ERR_UNSUPPORTED;
     (*seqs)[i] = {cu_q[i], cu_k[i], (int32_t)Lq, (int32_t)Lk};
+    tiles += row_tiles((int32_t)Lq, Hq / Hkv, 256);
+    keys += (Lk + 127) / 128;
   }
-  return UPIPE_OK;
+  // Before their lists are made, which may be more than the host's memory holds.
+  return grid_fits(tiles * Hkv, 512) && grid_fits(keys * Hkv, 256) ? UPIPE_OK
+                                                                   : UPIPE_ERR_UNSUPPORTED;
 }
 
 struct Plan {

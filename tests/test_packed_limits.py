@@ -2,6 +2,7 @@
 its threads in 32 bits."""
 
 import ctypes
+import time
 
 from paper_2602_21196_amd import upipe
 
@@ -28,3 +29,16 @@ def test_rows_of_caches():
     assert _decode(65535, 2, 64, 8) > 0 and _decode(65536, 2, 64, 8) == 0
     assert _decode(65536, 1, 64, 8) > 0
     assert _decode(65471, 1, 64, 8, P=1) > 0 and _decode(65472, 1, 64, 8, P=1) == 0
+
+
+def test_lengths_beyond_any_launch_are_refused_at_once():
+    """4096 sequences of the longest length, and keys alone: no list of their work is made
+    first (of 16 million tiles a sequence, some terabytes)."""
+    most = (1 << 24) - 128
+    long = [most * i for i in range(4097)]
+    none = [0] * 4097
+    for cu_q, cu_k, Hq in ((long, long, 64), (none, long, 64), (long, none, 1)):
+        q, k = ((ctypes.c_int64 * 4097)(*c) for c in (cu_q, cu_k))
+        start = time.process_time()
+        assert upipe.upipe_varlen_plan_size(q, k, 4096, Hq, 1, D, 1) == 0
+        assert time.process_time() - start < 0.1
