@@ -336,8 +336,8 @@ int upipe_attn_fwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_hea
  * span less than 2^30 bytes (UPIPE_ERR_UNSUPPORTED).  P and dS are rounded to bf16 for
  * their products, every sum is fp32 in a fixed order.  A masked pair's infinite or NaN
  * row of q, k or dout may reach the gradients of the pair's other row where the key lies
- * less than 192 behind the last one that the query sees.  The weights are formed again from scores and lse in fp32: they keep
- * digits for scores up to about 2^20. */
+ * less than 192 behind the last one that the query sees.  The weights are formed again from
+ * scores and lse in fp32: they keep digits for scores up to about 2^20. */
 size_t upipe_attn_bwd_varlen_workspace_size(const void* plan);
 int upipe_attn_bwd_varlen(upipe_heads q, upipe_heads k, upipe_heads v, upipe_heads o,
                           const float* lse, int64_t lse_head, upipe_heads dout, upipe_heads dq,

@@ -15,10 +15,10 @@
 // tensor's 16 weights (and its 16 sums of dw).  The angles are formed once per token and
 // pair of heads, in fp64 turns (positions to 2^32) with the frequencies from the
 // kernel's arguments.  The norm's sums, r, the rotation and the sums of dw are fp32; y,
-// dx and a bf16 dw are rounded once.  65536 tokens: 40 heads forward 247 - 252 us (5.3 - 5.4 TB/s,
-// a large copy 5.1), 72 heads backward 690 - 708 us (5.1 - 5.2 TB/s; a head at a time 742); 4000 tokens, 40
-// heads 17 and 27 us (before the weights came by wide loads and without 64-bit divisions
-// 22 and 31).
+// dx and a bf16 dw are rounded once.  65536 tokens: 40 heads forward 247 - 252 us (5.3 - 5.4
+// TB/s, a large copy 5.1), 72 heads backward 690 - 708 us (5.1 - 5.2 TB/s; a head at a time
+// 742); 4000 tokens, 40 heads 17 and 27 us (before the weights came by wide loads and
+// without 64-bit divisions 22 and 31).
 #include "common.h"
 #include "kernels.h"
 

@@ -261,11 +261,11 @@ __device__ __forceinline__ void careful_row(const bf16* k, int64_t k_row, const 
 // Infinite or not a number.
 __device__ __forceinline__ bool odd(float x) { return !(fabsf(x) < INFINITY); }
 
-// The odd elements of the wave's rows: what the odd visible values of their column add up
-// to, +-inf or not a number; that is the result, whatever the weights and the finite values.
-// The wave goes through the keys that all of its rows see, key0 .. common - 1, two columns
-// a lane, a row through its rest, to key1.  Returns whether an element is left whose visible
-// values are all finite, which it looks for in rows with `mine`.
+// The odd elements of the rows with `mine`: what the odd visible values of their column add
+// up to, +-inf or not a number; that is the result, whatever the weights and the finite
+// values.  The wave goes through the keys that all of its rows see, key0 .. common - 1, two
+// columns a lane, a row through its rest, to key1.  Returns whether an element is left
+// whose visible values are all finite.
 __device__ __forceinline__ int settle_columns(const bf16* v, int64_t v_row, int key0, int common,
                                               int key1, bool mine, f32x16 (&oacc)[4]) {
   const int lane = threadIdx.x & 63, g = lane >> 5;
@@ -290,19 +290,18 @@ __device__ __forceinline__ int settle_columns(const bf16* v, int64_t v_row, int 
 #pragma unroll 1
   for (; j0 < common; ++j0, p += v_row) take(*reinterpret_cast<const uint32_t*>(p));
   constexpr float OPEN = 3.4028235e38f;      // an odd element whose visible values are not, so far
-  const float open = mine ? OPEN : NAN;
 #pragma unroll
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       // of column 32 dt + 8 (i / 4) + 4 g + i % 4
       const float c = __shfl(sum[i & 1], 16 * dt + 4 * (i >> 2) + 2 * g + ((i & 3) >> 1));
-      oacc[dt][i] = odd(oacc[dt][i]) ? odd(c) ? c : open : oacc[dt][i];
+      oacc[dt][i] = mine && odd(oacc[dt][i]) ? odd(c) ? c : OPEN : oacc[dt][i];
       // (a condition is a pair of scalar registers: those of 64 elements would spill)
       if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll 1
-  for (int j = rest; j < key1; ++j) {
+  for (int j = rest; j < key1 && mine; ++j) {
     const bf16* vp = v + j * v_row + 4 * g;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -322,7 +321,7 @@ __device__ __forceinline__ int settle_columns(const bf16* v, int64_t v_row, int 
   for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) least = fminf(least, fabsf(oacc[dt][i] - OPEN));
-  return least == 0.f;
+  return mine && least == 0.f;
 }
 
 // A masked key's weight is 0, but the matrix instructions also multiply that 0 by the
